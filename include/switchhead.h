@@ -41,7 +41,7 @@ extern "C" {
 
 typedef struct sh_layer sh_layer;
 
-enum { SH_F32 = 0, SH_BF16 = 1 };
+enum { SH_F32 = 0, SH_BF16 = 1, SH_F16 = 2 };   /* (SH_F16: the operators of a training step only) */
 
 enum {
   SH_OK = 0,
@@ -270,6 +270,108 @@ int sh_noalloc_gate_topk(int dtype, int n_tokens, int d_model, int n_heads, int 
  * any order, so two calls agree to rounding, not bit for bit.  Work enqueued on `stream`. */
 int sh_backward(sh_layer* layer, const void* x, const float* dout, float* dx, float* dWq, float* dWk,
                 float* dWv, float* dWo, float* dWs, float* dWd, void* stream);
+
+/* ---- Operators of a training step around the projections and the selection ----
+ * They need no layer handle and own nothing.  Each call takes one struct of arguments, which is read before the
+ * call returns; the device must be the current one.  None of them reads a value on the host: all can be
+ * captured into a graph.  A workspace is scratch of one call at a time: two calls that may run at once (two streams,
+ * two graphs that are replayed side by side) want one each; nothing in it is kept or needs clearing. */
+
+/* The heads of queries, keys or their gradients: element (b, t, h, i) at data[b*batch_stride + t*token_stride +
+ * h*head_stride + i] - columns of a fused projection, [B, T, H, D], the layer's [B, H, T, D].  Strides in elements. */
+typedef struct {
+  void* data;
+  int64_t batch_stride, token_stride, head_stride;
+  int32_t heads, reserved;
+} sh_heads;
+
+/* Norms of queries and keys for each head, with the position rotation in the same pass.  For every row x of d_head values
+ * (a token's head):
+ *   n = g o x / sqrt(mean(x^2) + eps),   y = Rot(position) n   (queries: times q_scale)
+ * Rot turns the pair i < rotated/2 of the first `rotated` columns by position * base^(-2i/rotated): the columns (2i, 2i+1), as
+ * sh_set_rope does, or with halves != 0 the columns (i, i + rotated/2).  rotated = 0: no rotation.  Statistics in fp32, one rounding to
+ * the stored type.  Angles are exact to 2^-24 turns at every position a 32-bit integer holds.
+ *   dtype      of q, k, their outputs and gradients: SH_F32, SH_BF16 or SH_F16
+ *   q, k       heads may be 0 (that side is left out), and need not be equal (grouped heads)
+ *   q_out, k_out   the normalised and rotated heads (sh_qk_norm), or the gradients of q and k (sh_qk_norm_backward); their
+ *              `heads` is ignored.  May be q and k themselves (same strides), or dq and dk; otherwise no overlap.
+ *   gq, gk     [d_head] fp32 gains, shared by a side's heads; NULL: ones
+ *   positions  [batch, seq] int32 (positions_64 != 0: int64), any values; NULL: token t of a sequence is at position t
+ *   d_head 1..256, even with a rotation; eps positive.
+ * Backward (q, k: the inputs of the forward call; dq, dk: the gradients of its outputs): writes the gradients of q and k to
+ * q_out, k_out and those of the gains, summed over tokens and heads, to dgq, dgk [d_head] fp32 (NULL: not wanted; a sum over no
+ * rows is zero).  The workspace, sh_qk_norm_workspace_bytes(d_head) bytes aligned to 256, is wanted with dgq or dgk.
+ * The same inputs give the same bits. */
+typedef struct {
+  sh_heads q, k, q_out, k_out, dq, dk;
+  const float *gq, *gk;
+  float *dgq, *dgk;
+  const void* positions;
+  void* workspace;
+  size_t workspace_bytes;
+  double base;
+  int32_t dtype, batch, seq, d_head, rotated, halves, positions_64;
+  float eps, q_scale;
+  int32_t reserved;
+} sh_qk_norm_args;
+int sh_qk_norm(const sh_qk_norm_args* args, void* stream);
+int sh_qk_norm_backward(const sh_qk_norm_args* args, void* stream);
+size_t sh_qk_norm_workspace_bytes(int d_head);
+
+/* Balance loss of the gates, with the per-expert counts.  logits [N, sides, H, E] fp32 or bf16 (a token's gates dense, tokens
+ * token_stride elements apart), idx [sides, N, H, k] the selections (sh_gate_topk's layout), mask [N] bytes, zero: the token
+ * does not count (padding; its logits may be anything), or NULL.  Per gate, over the n tokens that count:
+ *   p = softmax(logits),  prob = P = mean of p,  counts = selections of each expert,  f = counts / their sum
+ *   SH_BALANCE_COUNTS:   loss = coef * sum over the gates of  E * sum_e f_e P_e        (1 a gate where all are used alike)
+ *   SH_BALANCE_ENTROPY:  loss = coef * sum over the gates of  sum_e P_e ln P_e         (the negative entropy of the mean)
+ * A negative entry of idx (or one that is no expert) is not counted.  A row of -inf only has p = 0.  No token that counts:
+ * everything is zero.
+ *   loss [1], prob, slope [sides, H, E] fp32, counts [sides, H, E] int32; slope = dloss/dprob / n, less its mean over the
+ *   gate's experts (which changes no gradient), is what sh_balance_backward reads.
+ * sh_balance_backward: dlogits = *gloss * dloss/dlogits (gloss: device, NULL: 1), in the type of the logits, tokens
+ * dtoken_stride elements apart; the counts are constants of it.  Tokens that do not count get zeros.  Reads logits, mask,
+ * slope; dlogits may be logits itself (same stride).
+ * workspace: sh_balance_workspace_bytes(sides, H, E) bytes aligned to 256 (sh_balance_loss only).  1 <= k <= E <= 32; N * k
+ * below 2^31.  The same inputs give the same bits. */
+enum { SH_BALANCE_COUNTS = 0, SH_BALANCE_ENTROPY = 1 };
+typedef struct {
+  int64_t n_tokens, token_stride, dtoken_stride;
+  const void* logits;
+  const int32_t* idx;
+  const void* mask;
+  const float* gloss;
+  float *loss, *prob, *slope;
+  int32_t* counts;
+  void* dlogits;
+  void* workspace;
+  size_t workspace_bytes;
+  int32_t dtype, kind, sides, n_heads, n_experts, k;
+  float coef;
+  int32_t reserved;
+} sh_balance_args;
+int sh_balance_loss(const sh_balance_args* args, void* stream);
+int sh_balance_backward(const sh_balance_args* args, void* stream);
+size_t sh_balance_workspace_bytes(int sides, int n_heads, int n_experts);
+
+/* Dropout: y[r, c] = residual[r, c] + (kept(r, c) ? x[r, c] / (1 - p) : 0) over a matrix of rows x cols (rows x_stride, y_stride,
+ * residual_stride elements apart; residual NULL: none).  The mask is never stored: it depends on the seed, the offset, r and c
+ * alone, so the gradient with respect to x is the same call on the gradient of y without a residual.
+ *   rng   DEVICE pointer to two uint64 {seed, offset}, read when the kernel runs: a captured call gives a new mask where the
+ *         offset has been changed.  Calls with other offsets (one a site and step) have independent masks.
+ *   kept  16 bits of Philox4x32-10 (Salmon et al. 2011), key = seed, counter = (c / 8, r, offset low, offset high), word
+ *         (c % 8) / 2, its lower half for an even c, are not below round(65536 p): p is taken to the nearest 2^-16 and the
+ *         factor is that of the p that is taken.
+ * dtype SH_F32, SH_BF16 or SH_F16; 0 <= p <= 1 (1: nothing is kept).  A dropped value does not count whatever it is (NaN).
+ * y may be x or residual (same stride). */
+typedef struct {
+  const void *x, *residual;
+  void* y;
+  const void* rng;
+  int64_t rows, cols, x_stride, residual_stride, y_stride;
+  double p;
+  int32_t dtype, reserved;
+} sh_dropout_args;
+int sh_dropout(const sh_dropout_args* args, void* stream);
 
 /* Device pointer and size of an intermediate buffer inside the workspace (contents are
  * those of the last sh_forward / sh_gate_topk once the stream has drained).  Element type:

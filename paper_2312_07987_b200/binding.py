@@ -7,7 +7,9 @@ There is no CPU fallback: if the library cannot be loaded, importing this module
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
+import struct
 from typing import Optional
 
 import numpy as np
@@ -15,7 +17,8 @@ import torch
 
 from . import build as _build
 
-SH_F32, SH_BF16 = 0, 1
+SH_F32, SH_BF16, SH_F16 = 0, 1, 2
+SH_BALANCE = dict(counts=0, entropy=1)
 SH_OK = 0
 ERROR_NAMES = {-1: "SH_ERR_INVALID_ARG", -2: "SH_ERR_UNSUPPORTED", -3: "SH_ERR_NOT_CONFIGURED",
                -4: "SH_ERR_WORKSPACE", -5: "SH_ERR_CUDA", -6: "SH_ERR_TIMEOUT", -7: "SH_ERR_BOUNDS"}
@@ -24,7 +27,9 @@ BUF = dict(Q=0, K=1, V=2, AHAT=3, IDX=4, GATE=5, OFFSETS=6, LISTS=7)
 EXPORTS = ["sh_create", "sh_create_shared", "sh_create_moe_qk", "sh_create_dense", "sh_configure", "sh_configure_xl", "sh_workspace_bytes", "sh_set_workspace",
            "sh_set_weights", "sh_set_causal", "sh_set_rope", "sh_set_xl_positions", "sh_forward", "sh_backward", "sh_forward_timed", "sh_forward_stamped", "sh_gate_topk",
            "sh_noalloc_gate_topk", "sh_debug_buffer", "sh_last_status", "sh_status_block", "sh_clear_status", "sh_check_guards",
-           "sh_selftest", "sh_set_output_f16", "sh_is_debug_build", "sh_launch_count", "sh_last_error", "sh_destroy"]
+           "sh_selftest", "sh_set_output_f16", "sh_is_debug_build", "sh_launch_count", "sh_last_error", "sh_destroy",
+           "sh_qk_norm", "sh_qk_norm_backward", "sh_qk_norm_workspace_bytes", "sh_balance_loss", "sh_balance_backward",
+           "sh_balance_workspace_bytes", "sh_dropout"]
 STAMP_KERNELS = ["gate", "sort", "qk_a", "qk_b", "v", "attn", "o"]
 
 
@@ -90,6 +95,13 @@ def _load() -> ctypes.CDLL:
     lib.sh_launch_count.argtypes = [vp]
     lib.sh_last_error.restype = ctypes.c_char_p
     lib.sh_last_error.argtypes = []
+    for name in ("sh_qk_norm", "sh_qk_norm_backward", "sh_balance_loss", "sh_balance_backward", "sh_dropout"):
+        getattr(lib, name).restype = i32
+        getattr(lib, name).argtypes = [ctypes.c_char_p, vp]      # a packed struct of arguments; the stream
+    lib.sh_qk_norm_workspace_bytes.restype = sz
+    lib.sh_qk_norm_workspace_bytes.argtypes = [i32]
+    lib.sh_balance_workspace_bytes.restype = sz
+    lib.sh_balance_workspace_bytes.argtypes = [i32] * 3
     lib.sh_destroy.restype = None
     lib.sh_destroy.argtypes = [vp]
     return lib
@@ -288,6 +300,196 @@ def sh_noalloc_gate_topk(dtype: int, x: torch.Tensor, w_gate: torch.Tensor, bias
     _check(lib.sh_noalloc_gate_topk(dtype, N, M, n_heads, n_experts, k, _ptr(x), _ptr(w_gate), _ptr(bias),
                                     _ptr(idx), _ptr(gate), _ptr(offsets), _ptr(lists), _stream()))
     return idx, gate, offsets, lists
+
+
+# The operators of a training step (switchhead.h).  Their arguments are one C struct, packed here field by field.
+_HEADS = "P3q2i"
+_QK_NORM = struct.Struct(_HEADS * 6 + "6PQd7i2fi")
+_BALANCE = struct.Struct("3q10PQ6ifi")
+_DROPOUT = struct.Struct("4P5qd2i")
+_DTYPES = {torch.float32: SH_F32, torch.bfloat16: SH_BF16, torch.float16: SH_F16}
+
+
+def _launch(fn, packed: bytes, device: torch.device) -> None:
+    """The call on the tensors' device and on the stream that is current there."""
+    if device.index == torch.cuda.current_device():
+        _check(fn(packed, torch.cuda.current_stream(device).cuda_stream))
+    else:
+        with torch.cuda.device(device):
+            _check(fn(packed, torch.cuda.current_stream(device).cuda_stream))
+
+
+def _refuse_unless(ok: bool, message: str) -> None:
+    if not ok:
+        raise ValueError(message)
+
+
+def _heads(name: str, t: Optional[torch.Tensor], like: torch.Tensor, shape) -> tuple:
+    """The fields of one sh_heads: t [B, T, heads, d_head], the last dimension dense."""
+    if t is None:
+        return (0, 0, 0, 0, 0, 0)
+    st = t.stride()
+    if t.shape != shape or t.dtype != like.dtype or t.device != like.device or (st[3] != 1 and shape[3] > 1):
+        raise ValueError(f"{name} must be [batch, seq, heads, d_head] = {tuple(shape)} of {like.dtype} on {like.device}, its last dimension "
+                         f"dense: got {tuple(t.shape)}, {t.dtype}, {t.device}, strides {tuple(st)}")
+    return (t.data_ptr(), st[0], st[1], st[2], shape[2], 0)
+
+
+def _dense_f32(name: str, t: Optional[torch.Tensor], like: torch.Tensor, shape) -> int:
+    if t is None:
+        return 0
+    if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or t.device != like.device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous fp32 tensor {tuple(shape)} on {like.device}: got {tuple(t.shape)}, {t.dtype}, {t.device}")
+    return t.data_ptr()
+
+
+def _qk_norm_pack(q, k, q_out, k_out, dq, dk, gq, gk, dgq, dgk, workspace, eps, base, rotated, halves, positions, q_scale) -> bytes:
+    shape = q.shape
+    if q.dim() != 4 or q.dtype not in _DTYPES or not q.is_cuda:
+        raise ValueError(f"q must be a CUDA tensor [batch, seq, heads, d_head] of fp32, bf16 or fp16: got {tuple(shape)}, {q.dtype}, {q.device}")
+    ks = None
+    if k is not None:
+        ks = k.shape
+        if k.dim() != 4 or ks[0] != shape[0] or ks[1] != shape[1] or ks[3] != shape[3]:
+            raise ValueError(f"k must be [batch, seq, heads, d_head] with q's batch, seq and d_head: got {tuple(ks)}, q {tuple(shape)}")
+    pos = 0
+    if positions is not None:
+        if positions.shape != shape[:2] or positions.dtype not in (torch.int32, torch.int64) or positions.device != q.device or not positions.is_contiguous():
+            raise ValueError(f"positions must be a contiguous int32 or int64 tensor {tuple(shape[:2])} on {q.device}: got {tuple(positions.shape)}, {positions.dtype}, {positions.device}")
+        pos = positions.data_ptr()
+    D = shape[3]
+    one = (D,)
+    return _QK_NORM.pack(*_heads("q", q, q, shape), *_heads("k", k, q, ks), *_heads("the output for q", q_out, q, shape), *_heads("the output for k", k_out, q, ks),
+                         *_heads("dq", dq, q, shape), *_heads("dk", dk, q, ks), _dense_f32("gq", gq, q, one), _dense_f32("gk", gk, q, one),
+                         0 if dgq is None else dgq.data_ptr(), 0 if dgk is None else dgk.data_ptr(), pos,
+                         0 if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(), base,
+                         _DTYPES[q.dtype], shape[0], shape[1], D, rotated, 1 if halves else 0, 1 if pos and positions.dtype == torch.int64 else 0, eps, q_scale, 0)
+
+
+def sh_qk_norm(q: torch.Tensor, k: Optional[torch.Tensor], gq: Optional[torch.Tensor] = None, gk: Optional[torch.Tensor] = None, *, eps: float = 1e-6,
+               base: float = 10000.0, rotated: int = 0, halves: bool = False, positions: Optional[torch.Tensor] = None, q_scale: float = 1.0,
+               q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """Queries and keys normalised per head and rotated by their position, in one pass.  q, k [batch, seq, heads, d_head] in any strides
+    with a dense last dimension (columns of a fused projection, transposed views); k may be None.  gq, gk [d_head] fp32 gains.
+    q_out, k_out: where the results go (q and k themselves are allowed).  Returns (q_out, k_out)."""
+    if q_out is None:
+        q_out = torch.empty_like(q)
+    if k_out is None and k is not None:
+        k_out = torch.empty_like(k)
+    _launch(lib.sh_qk_norm, _qk_norm_pack(q, k, q_out, k_out, None, None, gq, gk, None, None, None, eps, base, rotated, halves, positions, q_scale), q.device)
+    return q_out, k_out
+
+
+@functools.lru_cache(maxsize=None)
+def _qk_norm_workspace_bytes(d_head: int) -> int:
+    return lib.sh_qk_norm_workspace_bytes(d_head)
+
+
+@functools.lru_cache(maxsize=None)
+def _balance_workspace_bytes(sides: int, heads: int, experts: int) -> int:
+    return lib.sh_balance_workspace_bytes(sides, heads, experts)
+
+
+def sh_qk_norm_backward(q: torch.Tensor, k: Optional[torch.Tensor], dq: torch.Tensor, dk: Optional[torch.Tensor], gq: Optional[torch.Tensor] = None,
+                        gk: Optional[torch.Tensor] = None, *, eps: float = 1e-6, base: float = 10000.0, rotated: int = 0, halves: bool = False,
+                        positions: Optional[torch.Tensor] = None, q_scale: float = 1.0) -> dict:
+    """Gradients of sh_qk_norm(q, k, gq, gk, ...) from those of its outputs, dq and dk: {dq, dk} with respect to its inputs, and of the
+    gains that were given (dgq, dgk [d_head] fp32, summed over tokens and heads; None where there is no gain)."""
+    _refuse_unless(dq is not None and (dk is None) == (k is None), "dq and, with k, dk must be given")
+    out_q, out_k = torch.empty_like(q), None if k is None else torch.empty_like(k)
+    D = q.shape[-1]
+    dgq = None if gq is None else torch.empty(D, dtype=torch.float32, device=q.device)
+    dgk = None if gk is None else torch.empty(D, dtype=torch.float32, device=q.device)
+    ws = None if gq is None and gk is None else torch.empty(_qk_norm_workspace_bytes(D), dtype=torch.uint8, device=q.device)
+    _launch(lib.sh_qk_norm_backward, _qk_norm_pack(q, k, out_q, out_k, dq, dk, gq, gk, dgq, dgk, ws, eps, base, rotated, halves, positions, q_scale), q.device)
+    return dict(dq=out_q, dk=out_k, dgq=dgq, dgk=dgk)
+
+
+def _logits(name: str, z: torch.Tensor) -> None:
+    """[N, sides, heads, experts] with a token's gates dense."""
+    s, st = z.shape, z.stride()
+    if (z.dim() != 4 or z.dtype not in (torch.float32, torch.bfloat16) or not z.is_cuda
+            or not ((s[3] == 1 or st[3] == 1) and (s[2] == 1 or st[2] == s[3]) and (s[1] == 1 or st[1] == s[2] * s[3]))):
+        raise ValueError(f"{name} must be a CUDA tensor [tokens, sides, heads, experts] of fp32 or bf16, a token's gates dense: got {tuple(s)}, {z.dtype}, {z.device}, strides {z.stride()}")
+
+
+def _token_mask(mask: Optional[torch.Tensor], z: torch.Tensor) -> int:
+    if mask is None:
+        return 0
+    if mask.dtype not in (torch.bool, torch.uint8) or mask.shape != z.shape[:1] or mask.device != z.device or not mask.is_contiguous():
+        raise ValueError(f"mask must be a contiguous bool or uint8 tensor [{z.shape[0]}] on {z.device}: got {tuple(mask.shape)}, {mask.dtype}, {mask.device}")
+    return mask.data_ptr()
+
+
+def sh_balance_loss(logits: torch.Tensor, idx: torch.Tensor, *, kind: str = "counts", coef: float = 1.0, mask: Optional[torch.Tensor] = None) -> dict:
+    """Balance loss of the gates with the per-expert counts.  logits [N, sides, heads, experts] fp32 or bf16; idx [sides, N, heads, k] int32 (the
+    selections, as sh_gate_topk gives them); mask [N]: tokens that count.  Returns {loss, counts, prob, slope}: loss a scalar, the others
+    [sides, heads, experts]; slope is what sh_balance_backward takes."""
+    _logits("logits", logits)
+    N, S, H, E = logits.shape
+    if idx.dtype != torch.int32 or idx.dim() != 4 or idx.shape[:3] != (S, N, H) or idx.device != logits.device or not idx.is_contiguous():
+        raise ValueError(f"idx must be a contiguous int32 tensor [sides, tokens, heads, k] on {logits.device}: got {tuple(idx.shape)}, {idx.dtype}, {idx.device}")
+    if kind not in SH_BALANCE:
+        raise ValueError(f"kind must be one of {sorted(SH_BALANCE)}: got {kind!r}")
+    dev = logits.device
+    loss = torch.empty((), dtype=torch.float32, device=dev)
+    prob = torch.empty((S, H, E), dtype=torch.float32, device=dev)
+    slope = torch.empty((S, H, E), dtype=torch.float32, device=dev)
+    counts = torch.empty((S, H, E), dtype=torch.int32, device=dev)
+    nbytes = _balance_workspace_bytes(S, H, E)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _launch(lib.sh_balance_loss, _BALANCE.pack(N, logits.stride(0), 0, logits.data_ptr(), idx.data_ptr(), _token_mask(mask, logits), 0, loss.data_ptr(),
+                                               prob.data_ptr(), slope.data_ptr(), counts.data_ptr(), 0, ws.data_ptr(), nbytes,
+                                               _DTYPES[logits.dtype], SH_BALANCE[kind], S, H, E, idx.shape[3], coef, 0), dev)
+    return dict(loss=loss, counts=counts, prob=prob, slope=slope)
+
+
+def sh_balance_backward(logits: torch.Tensor, slope: torch.Tensor, *, gloss: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient of the balance loss with respect to the logits, times gloss (a device scalar, the gradient of the loss); slope and mask: of the
+    sh_balance_loss call.  out: where it goes (logits itself is allowed)."""
+    _logits("logits", logits)
+    N, S, H, E = logits.shape
+    if out is None:
+        out = torch.empty((N, S, H, E), dtype=logits.dtype, device=logits.device)
+    elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device:
+        raise ValueError("out must have the shape, type and device of logits")
+    else:
+        _logits("out", out)
+    _launch(lib.sh_balance_backward, _BALANCE.pack(N, logits.stride(0), out.stride(0), logits.data_ptr(), 0, _token_mask(mask, logits),
+                                                   _dense_f32("gloss", gloss, logits, ()),
+                                                   0, 0, _dense_f32("slope", slope, logits, (S, H, E)), 0, out.data_ptr(), 0, 0,
+                                                   _DTYPES[logits.dtype], 0, S, H, E, 1, 0.0, 0), logits.device)
+    return out
+
+
+def sh_dropout(x: torch.Tensor, rng: torch.Tensor, p: float, *, residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """residual + dropout(x) over rows of x's last dimension, fp32, bf16 or fp16.  rng: a device tensor of two int64, the seed and the offset (another
+    offset for every site and step); the mask follows from them alone, so sh_dropout(dy, rng, p) is the gradient's way back.
+    out may be x or residual."""
+    if x.dtype not in _DTYPES or not x.is_cuda or x.dim() < 1:
+        raise ValueError(f"x must be a CUDA tensor [..., columns] of fp32, bf16 or fp16: got {tuple(x.shape)}, {x.dtype}, {x.device}")
+    if rng.dtype != torch.int64 or tuple(rng.shape) != (2,) or rng.device != x.device or not rng.is_contiguous():
+        raise ValueError(f"rng must be a contiguous int64 tensor [2] on {x.device}: got {tuple(rng.shape)}, {rng.dtype}, {rng.device}")
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    cols = x.shape[-1]
+    rows = x.numel() // cols if cols else 0
+
+    def stride(name, t):
+        if t.shape != x.shape or t.dtype != x.dtype or t.device != x.device:
+            raise ValueError(f"{name} must have the shape, type and device of x")
+        if t.is_contiguous():
+            return cols
+        if t.dim() == 2 and (t.stride(1) == 1 or cols == 1):
+            return t.stride(0)
+        raise ValueError(f"{name} must be contiguous, or a matrix with dense rows")
+
+    xs, ys = stride("x", x), stride("out", out)
+    rs = 0 if residual is None else stride("residual", residual)
+    _launch(lib.sh_dropout, _DROPOUT.pack(x.data_ptr(), 0 if residual is None else residual.data_ptr(), out.data_ptr(), rng.data_ptr(),
+                                          rows, cols, xs, rs, ys, p, _DTYPES[x.dtype], 0), x.device)
+    return out
 
 
 def to_device(a: Optional[np.ndarray], dtype: int, device="cuda") -> Optional[torch.Tensor]:

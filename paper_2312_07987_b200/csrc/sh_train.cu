@@ -1,0 +1,398 @@
+// Operators of a training step around the layer's projections and its selection: norms of queries and keys with the
+// position rotation (sh_qknorm.cuh), the balance loss of the gates (sh_balance.cuh), dropout (sh_dropout.cuh).
+// Argument checks and launches; every entry point is documented in include/switchhead.h.
+#include <cmath>
+#include <initializer_list>
+#include <utility>
+
+#include "sh_launch.cuh"
+#include "sh_qknorm.cuh"
+#include "sh_balance.cuh"
+#include "sh_dropout.cuh"
+
+namespace {
+
+size_t elem_bytes(int dtype) { return dtype == SH_F32 ? 4 : 2; }
+
+bool dtype_ok(int dtype, bool f16) {
+  if (dtype == SH_F32 || dtype == SH_BF16 || (f16 && dtype == SH_F16)) return true;
+  sh_set_error(f16 ? "dtype must be SH_F32, SH_BF16 or SH_F16 (got %d)" : "dtype must be SH_F32 or SH_BF16 (got %d)", dtype);
+  return false;
+}
+
+// SMs of the current device.
+int device_sms(int* n) {
+  static int sms[64];                                      // (an SM count is written once or several times with the same value)
+  int dev = 0;
+  SH_CUDA_CHECK(cudaGetDevice(&dev));
+  int v = dev < 64 ? __atomic_load_n(&sms[dev], __ATOMIC_RELAXED) : 0;
+  if (v == 0) {
+    SH_CUDA_CHECK(cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev));
+    if (dev < 64) __atomic_store_n(&sms[dev], v, __ATOMIC_RELAXED);
+  }
+  *n = v;
+  return SH_OK;
+}
+
+int pow2_at_least(int n) { int p = 1; while (p < n) p *= 2; return p; }
+
+// ---- norms of queries and keys ----
+
+bool heads_ok(const char* what, const sh_heads& h) {
+  if (h.heads < 0) { sh_set_error("%s: heads must not be negative (got %d)", what, h.heads); return false; }
+  if (h.heads > 0 && !h.data) { sh_set_error("%s: data must not be NULL", what); return false; }
+  return true;
+}
+
+// Two elements of an output at one address: a dimension of more than one has no stride.
+bool apart(const char* what, std::initializer_list<std::pair<long long, long long>> dims) {
+  for (auto& d : dims)
+    if (d.first > 1 && d.second == 0) { sh_set_error("%s: elements of an output must not share an address (stride 0)", what); return false; }
+  return true;
+}
+
+// Values a vector may have: every address and every run of columns is a multiple of it.
+int vector_width(const sh_qk_norm_args& a, bool backward) {
+  const int size = (int)elem_bytes(a.dtype);
+  int v = 16 / size;
+  auto fits = [&](long long n) { while (v > 1 && n % v) v /= 2; };
+  fits(a.d_head);
+  if (a.rotated && a.halves) { fits(a.rotated / 2); fits((a.d_head - a.rotated) / 2); }
+  const sh_heads* t[] = {&a.q, &a.k, &a.q_out, &a.k_out, &a.dq, &a.dk};
+  for (int i = 0; i < (backward ? 6 : 4); ++i) {
+    const sh_heads& h = *t[i];
+    const int heads = i % 2 ? a.k.heads : a.q.heads;
+    if (heads == 0) continue;
+    fits((long long)((uintptr_t)h.data / size));
+    if (a.batch > 1) fits(h.batch_stride);
+    if (a.seq > 1) fits(h.token_stride);
+    if (heads > 1) fits(h.head_stride);
+  }
+  return v;
+}
+
+int qn_check(const sh_qk_norm_args* p, bool backward) {
+  sh_set_error("%s", "");
+  if (!p) { sh_set_error("args is NULL"); return SH_ERR_INVALID_ARG; }
+  const sh_qk_norm_args& a = *p;
+  if (!dtype_ok(a.dtype, true)) return SH_ERR_INVALID_ARG;
+  if (a.batch < 0 || a.seq < 0) { sh_set_error("batch and seq must not be negative (got %d, %d)", a.batch, a.seq); return SH_ERR_INVALID_ARG; }
+  if (a.d_head < 1 || a.d_head > QN_MAX_D) { sh_set_error("d_head must be in 1..%d (got %d)", QN_MAX_D, a.d_head); return SH_ERR_INVALID_ARG; }
+  if (a.rotated < 0 || a.rotated > a.d_head || a.rotated % 2) { sh_set_error("rotated must be even and in 0..d_head (got %d, d_head %d)", a.rotated, a.d_head); return SH_ERR_INVALID_ARG; }
+  if (a.rotated && a.d_head % 2) { sh_set_error("a rotation needs an even d_head (got %d)", a.d_head); return SH_ERR_UNSUPPORTED; }
+  if (a.rotated && !(a.base > 0.0 && std::isfinite(a.base))) { sh_set_error("rotary base must be positive and finite (got %g)", a.base); return SH_ERR_INVALID_ARG; }
+  if (!(a.eps > 0.f && std::isfinite(a.eps))) { sh_set_error("eps must be positive and finite (got %g)", (double)a.eps); return SH_ERR_INVALID_ARG; }
+  if (!std::isfinite(a.q_scale)) { sh_set_error("q_scale must be finite (got %g)", (double)a.q_scale); return SH_ERR_INVALID_ARG; }
+  if (a.batch == 0 || a.seq == 0) {
+    if (a.q.heads < 0 || a.k.heads < 0) { sh_set_error("heads must not be negative (got %d, %d)", a.q.heads, a.k.heads); return SH_ERR_INVALID_ARG; }
+    return SH_OK;
+  }
+  if (!heads_ok("q", a.q) || !heads_ok("k", a.k)) return SH_ERR_INVALID_ARG;
+  const sh_heads *oq = &a.q_out, *ok = &a.k_out;
+  if ((a.q.heads && !oq->data) || (a.k.heads && !ok->data)) { sh_set_error("q_out and k_out must not be NULL"); return SH_ERR_INVALID_ARG; }
+  if (a.q.heads && !apart("q_out", {{a.batch, oq->batch_stride}, {a.seq, oq->token_stride}, {a.q.heads, oq->head_stride}})) return SH_ERR_INVALID_ARG;
+  if (a.k.heads && !apart("k_out", {{a.batch, ok->batch_stride}, {a.seq, ok->token_stride}, {a.k.heads, ok->head_stride}})) return SH_ERR_INVALID_ARG;
+  if (backward && ((a.q.heads && !a.dq.data) || (a.k.heads && !a.dk.data))) { sh_set_error("dq and dk must not be NULL"); return SH_ERR_INVALID_ARG; }
+  return SH_OK;
+}
+
+// The kernel's arguments; `per` heads to a group.
+void qn_fill(const sh_qk_norm_args& p, bool backward, int v, int nv, QnArgs& a) {
+  const sh_heads* in[2] = {&p.q, &p.k};
+  const sh_heads* out[2] = {&p.q_out, &p.k_out};
+  const sh_heads* dy[2] = {&p.dq, &p.dk};
+  for (int i = 0; i < 2; ++i) {
+    QnSide& s = a.s[i];
+    s.x = in[i]->data; s.xb = in[i]->batch_stride; s.xt = in[i]->token_stride; s.xh = in[i]->head_stride;
+    s.out = out[i]->data; s.ob = out[i]->batch_stride; s.ot = out[i]->token_stride; s.oh = out[i]->head_stride;
+    s.dy = nullptr; s.yb = s.yt = s.yh = 0;
+    if (backward) { s.dy = dy[i]->data; s.yb = dy[i]->batch_stride; s.yt = dy[i]->token_stride; s.yh = dy[i]->head_stride; }
+    s.gain = i ? p.gk : p.gq;
+    s.dgain = backward ? (i ? p.dgk : p.dgq) : nullptr;
+    s.heads = in[i]->heads;
+    s.scale = i ? 1.f : p.q_scale;
+  }
+  a.pos = p.positions; a.pos64 = p.positions_64 != 0;
+  a.next = p.rotated && !p.halves;
+  a.seq = p.seq; a.D = p.d_head; a.R = p.rotated;
+  a.tokens = (long long)p.batch * p.seq;
+  a.eps = p.eps;
+  a.lanes = pow2_at_least((p.d_head + v * nv - 1) / (v * nv));
+  a.blocks0 = 0; a.part = nullptr;
+  // (frequencies by one multiplication each: 64 bits of mantissa, off by a few units of 2^-63 relative at the last)
+  if (p.rotated) {
+    const long double two_pi = 6.283185307179586476925286766559005768L, ratio = powl((long double)p.base, -2.0L / p.rotated);
+    long double f = 1.0L / two_pi;
+    for (int i = 0; i < p.rotated / 2; ++i, f *= ratio) a.freq[i] = (unsigned long long)((f - floorl(f)) * 18446744073709551616.0L);
+  }
+}
+
+template <typename T, int V, int NV, bool HALVES>
+int qn_launch(const QnArgs& a, bool backward, bool pdl, int blocks, size_t smem, cudaStream_t st) {
+  if (!backward) return launch_k(pdl, sh_qk_norm_kernel<T, V, NV, HALVES>, dim3((unsigned)blocks), dim3(QN_THREADS), 0, st, a);
+  return launch_k(pdl, sh_qk_norm_backward_kernel<T, V, NV, HALVES>, dim3((unsigned)blocks), dim3(QN_THREADS), smem, st, a);
+}
+
+constexpr int qn_vectors(int v) { return v >= 4 ? 2 : v == 2 ? 4 : 8; }
+
+template <typename T>
+int qn_dispatch(const QnArgs& a, int v, bool halves, bool backward, bool pdl, int blocks, size_t smem, cudaStream_t st) {
+  if constexpr (sizeof(T) == 2)
+    if (v == 8) return halves ? qn_launch<T, 8, 2, true>(a, backward, pdl, blocks, smem, st) : qn_launch<T, 8, 2, false>(a, backward, pdl, blocks, smem, st);
+  if (v >= 4) return halves ? qn_launch<T, 4, 2, true>(a, backward, pdl, blocks, smem, st) : qn_launch<T, 4, 2, false>(a, backward, pdl, blocks, smem, st);
+  if (v == 2) return halves ? qn_launch<T, 2, 4, true>(a, backward, pdl, blocks, smem, st) : qn_launch<T, 2, 4, false>(a, backward, pdl, blocks, smem, st);
+  // (nothing rotated: d_head may be odd)
+  return a.R ? qn_launch<T, 1, 8, true>(a, backward, pdl, blocks, smem, st) : qn_launch<T, 1, 8, false>(a, backward, pdl, blocks, smem, st);
+}
+
+int qn_run(const sh_qk_norm_args& p, bool backward, bool pdl, cudaStream_t st) {
+  int sms = 0;
+  if (int rc = device_sms(&sms)) return rc;
+  const bool halves = p.rotated && p.halves;
+  const int v = vector_width(p, backward);
+  QnArgs a;
+  qn_fill(p, backward, v, qn_vectors(v), a);
+  const int groups = QN_THREADS / a.lanes, most = p.q.heads > p.k.heads ? p.q.heads : p.k.heads;
+  // heads to a group: all of them share a token's angles, but not so many that SMs are left without work
+  a.per = most < 8 ? (most < 1 ? 1 : most) : 8;
+  auto chunks = [&](int i) { return (a.s[i].heads + a.per - 1) / a.per; };
+  while (a.per > 1 && a.tokens * (chunks(0) + chunks(1)) < 4ll * sms * groups) a.per = a.per > 2 ? (a.per + 1) / 2 : 1;
+  a.s[0].chunks = chunks(0); a.s[1].chunks = chunks(1);
+  const long long items[2] = {a.tokens * a.s[0].chunks, a.tokens * a.s[1].chunks};
+  long long blocks = (items[0] + items[1] + groups - 1) / groups;
+  size_t smem = 0;
+  if (backward) {
+    long long n[2];
+    for (int i = 0; i < 2; ++i) n[i] = (items[i] + groups - 1) / groups;
+    const long long cap = 4ll * sms < QN_MAX_BLOCKS ? 4ll * sms : QN_MAX_BLOCKS;
+    if (n[0] + n[1] > cap) {                               // shares by the sides' rows
+      const long long all = n[0] + n[1];
+      const long long b0 = n[0] ? (n[0] * cap + all / 2) / all : 0;
+      n[0] = n[0] && b0 < 1 ? 1 : n[1] && b0 > cap - 1 ? cap - 1 : b0;
+      n[1] = n[1] ? cap - n[0] : 0;
+    }
+    a.blocks0 = (int)n[0];
+    blocks = n[0] + n[1];
+    a.part = (float*)p.workspace;
+    smem = (size_t)groups * p.d_head * 4;
+  }
+  if (blocks > 0x7fffffffll) { sh_set_error("too many rows: batch * seq * heads / %d must be below 2^31", groups); return SH_ERR_UNSUPPORTED; }
+  if (blocks) {
+    int rc = p.dtype == SH_F32 ? qn_dispatch<float>(a, v, halves, backward, pdl, (int)blocks, smem, st)
+           : p.dtype == SH_BF16 ? qn_dispatch<__nv_bfloat16>(a, v, halves, backward, pdl, (int)blocks, smem, st)
+                                : qn_dispatch<__half>(a, v, halves, backward, pdl, (int)blocks, smem, st);
+    if (rc) return rc;
+  }
+  if (backward && (p.dgq || p.dgk)) {
+    QnGain g{a.part, {p.dgq, p.dgk}, {0, a.blocks0, (int)blocks}, p.d_head};
+    return launch_k(blocks > 0, sh_qk_norm_gain_kernel, dim3((unsigned)((p.d_head + 31) / 32), 2), dim3(32, 32), 0, st, g);
+  }
+  return SH_OK;
+}
+
+
+// ---- balance loss ----
+
+struct BlPlan { int w, l, per, ny, tpb, nx; bool vec; };
+
+constexpr size_t kBlHead = 256;
+size_t bl_losses(long long gates) { return ((size_t)gates * 8 + 255) / 256 * 256; }
+
+// The thread layout for E logits of a gate; `vec`: rows are whole, aligned vectors.
+BlPlan bl_plan(int dtype, long long tokens, int gates, int E, bool aligned, int sms) {
+  BlPlan p;
+  p.w = dtype == SH_F32 || E <= 4 ? 4 : 8;
+  p.l = pow2_at_least((E + p.w - 1) / p.w);
+  p.vec = aligned && E == p.w * p.l;
+  const int rows = BL_THREADS / p.l;
+  p.ny = (gates + rows - 1) / rows;
+  p.per = (gates + p.ny - 1) / p.ny;
+  p.tpb = rows / p.per;
+  const long long rounds = (tokens + p.tpb - 1) / p.tpb;
+  long long cap = 4ll * sms < BL_MAX_BLOCKS ? 4ll * sms : BL_MAX_BLOCKS;
+  cap = cap / p.ny < 1 ? 1 : cap / p.ny;
+  p.nx = (int)(rounds < 1 ? 1 : rounds < cap ? rounds : cap);
+  return p;
+}
+
+bool bl_aligned(const void* z, long long stride, int gates, int E, int w, int size, long long tokens) {
+  const size_t bytes = (size_t)w * size;
+  return (uintptr_t)z % bytes == 0 && (tokens < 2 || (size_t)stride * size % bytes == 0) && (gates < 2 || (size_t)E * size % bytes == 0);
+}
+
+int bl_check(const sh_balance_args* p, bool backward) {
+  sh_set_error("%s", "");
+  if (!p) { sh_set_error("args is NULL"); return SH_ERR_INVALID_ARG; }
+  const sh_balance_args& a = *p;
+  if (!dtype_ok(a.dtype, false)) return SH_ERR_INVALID_ARG;
+  if (a.n_tokens < 0) { sh_set_error("n_tokens must not be negative (got %lld)", (long long)a.n_tokens); return SH_ERR_INVALID_ARG; }
+  if (a.sides < 1 || a.n_heads < 1 || a.n_experts < 1 || a.n_experts > 32) {
+    sh_set_error("sides and n_heads must be >= 1, n_experts in 1..32 (got %d, %d, %d)", a.sides, a.n_heads, a.n_experts);
+    return SH_ERR_INVALID_ARG;
+  }
+  const long long gates = (long long)a.sides * a.n_heads;
+  if (gates > 65535) { sh_set_error("sides * n_heads must be at most 65535 (got %lld)", gates); return SH_ERR_UNSUPPORTED; }
+  if (a.n_tokens && !a.logits) { sh_set_error("logits must not be NULL"); return SH_ERR_INVALID_ARG; }
+  if (backward) {
+    if (!a.slope || (a.n_tokens && !a.dlogits)) { sh_set_error("slope and dlogits must not be NULL"); return SH_ERR_INVALID_ARG; }
+    return apart("dlogits", {{a.n_tokens, a.dtoken_stride}}) ? SH_OK : SH_ERR_INVALID_ARG;
+  }
+  if (a.k < 1 || a.k > a.n_experts) { sh_set_error("k must be in 1..n_experts (got k=%d, n_experts=%d)", a.k, a.n_experts); return SH_ERR_INVALID_ARG; }
+  if (a.n_tokens >= (1ll << 31) / a.k) { sh_set_error("n_tokens * k must be below 2^31 (got %lld, %d)", (long long)a.n_tokens, a.k); return SH_ERR_UNSUPPORTED; }
+  if (a.kind != SH_BALANCE_COUNTS && a.kind != SH_BALANCE_ENTROPY) { sh_set_error("unknown kind of balance loss: %d", a.kind); return SH_ERR_INVALID_ARG; }
+  if (!std::isfinite(a.coef)) { sh_set_error("coef must be finite (got %g)", (double)a.coef); return SH_ERR_INVALID_ARG; }
+  if ((a.n_tokens && !a.idx) || !a.loss || !a.counts || !a.prob || !a.slope) { sh_set_error("idx, loss, counts, prob and slope must not be NULL"); return SH_ERR_INVALID_ARG; }
+  const size_t need = sh_balance_workspace_bytes(a.sides, a.n_heads, a.n_experts);
+  if (!a.workspace || (uintptr_t)a.workspace % 256) { sh_set_error("workspace must be a device pointer aligned to 256 bytes"); return SH_ERR_WORKSPACE; }
+  if (a.workspace_bytes < need) { sh_set_error("workspace too small: %zu bytes given, %zu needed", a.workspace_bytes, need); return SH_ERR_WORKSPACE; }
+  return SH_OK;
+}
+
+void bl_fill(const sh_balance_args& p, const BlPlan& pl, BlArgs& a) {
+  a.z = p.logits; a.dz = p.dlogits; a.idx = p.idx; a.mask = (const unsigned char*)p.mask;
+  a.slope = p.slope; a.gloss = p.gloss;
+  a.tokens = p.n_tokens; a.zt = p.token_stride; a.dzt = p.dtoken_stride;
+  a.gates = p.sides * p.n_heads; a.H = p.n_heads; a.E = p.n_experts; a.k = p.k;
+  a.per = pl.per; a.tpb = pl.tpb;
+  a.part_p = nullptr; a.part_n = nullptr; a.ticket = nullptr;
+}
+
+template <typename T, int W, int L, bool VEC>
+int bl_launch(const BlArgs& a, const BlPlan& p, int what, bool pdl, cudaStream_t st) {
+  const dim3 grid((unsigned)p.nx, (unsigned)p.ny);
+  if (what == 0) return launch_k(pdl, sh_balance_sums_kernel<T, W, L, VEC>, grid, dim3(BL_THREADS), 0, st, a);
+  if constexpr (sizeof(T) == 4)
+    if (what == 2) return launch_k(pdl, sh_balance_backward_kernel<T, W, L, VEC, true>, grid, dim3(BL_THREADS), 0, st, a);
+  return launch_k(pdl, sh_balance_backward_kernel<T, W, L, VEC, false>, grid, dim3(BL_THREADS), 0, st, a);
+}
+
+// what: 0 the sums, 1 dz, 2 dz added (fp32)
+int bl_dispatch(int dtype, const BlArgs& a, const BlPlan& p, int what, bool pdl, cudaStream_t st) {
+#define SH_BL(T, W, L) return p.vec ? bl_launch<T, W, L, true>(a, p, what, pdl, st) : bl_launch<T, W, L, false>(a, p, what, pdl, st)
+  if (dtype == SH_F32) {
+    if (p.l == 1) SH_BL(float, 4, 1);
+    if (p.l == 2) SH_BL(float, 4, 2);
+    if (p.l == 4) SH_BL(float, 4, 4);
+    SH_BL(float, 4, 8);
+  }
+  if (p.w == 4) SH_BL(__nv_bfloat16, 4, 1);
+  if (p.l == 1) SH_BL(__nv_bfloat16, 8, 1);
+  if (p.l == 2) SH_BL(__nv_bfloat16, 8, 2);
+  SH_BL(__nv_bfloat16, 8, 4);
+#undef SH_BL
+}
+
+BlPlan bl_plan_for(const sh_balance_args& p, bool backward, int sms) {
+  const int gates = p.sides * p.n_heads, size = (int)elem_bytes(p.dtype), w = p.dtype == SH_F32 || p.n_experts <= 4 ? 4 : 8;
+  bool aligned = bl_aligned(p.logits, p.token_stride, gates, p.n_experts, w, size, p.n_tokens);
+  if (backward) aligned = aligned && bl_aligned(p.dlogits, p.dtoken_stride, gates, p.n_experts, w, size, p.n_tokens);
+  return bl_plan(p.dtype, p.n_tokens, gates, p.n_experts, aligned, sms);
+}
+
+}  // namespace
+
+extern "C" int sh_qk_norm(const sh_qk_norm_args* args, void* stream) {
+  if (int rc = qn_check(args, false)) return rc;
+  if (args->batch == 0 || args->seq == 0) return SH_OK;
+  return qn_run(*args, false, false, (cudaStream_t)stream);
+}
+
+extern "C" size_t sh_qk_norm_workspace_bytes(int d_head) {
+  return d_head < 1 || d_head > QN_MAX_D ? 0 : (size_t)QN_MAX_BLOCKS * d_head * 4;
+}
+
+extern "C" int sh_qk_norm_backward(const sh_qk_norm_args* args, void* stream) {
+  if (int rc = qn_check(args, true)) return rc;
+  const sh_qk_norm_args& a = *args;
+  const size_t need = sh_qk_norm_workspace_bytes(a.d_head);
+  if (a.dgq || a.dgk) {
+    if (!a.workspace || (uintptr_t)a.workspace % 256) { sh_set_error("workspace must be a device pointer aligned to 256 bytes"); return SH_ERR_WORKSPACE; }
+    if (a.workspace_bytes < need) { sh_set_error("workspace too small: %zu bytes given, %zu needed", a.workspace_bytes, need); return SH_ERR_WORKSPACE; }
+  }
+  return qn_run(a, true, false, (cudaStream_t)stream);
+}
+
+extern "C" size_t sh_balance_workspace_bytes(int sides, int n_heads, int n_experts) {
+  const long long gates = (long long)sides * n_heads;
+  if (sides < 1 || n_heads < 1 || gates > 65535 || n_experts < 1 || n_experts > 32) return 0;
+  return kBlHead + bl_losses(gates) + (size_t)BL_MAX_BLOCKS * (gates * n_experts * 8 + 4);
+}
+
+extern "C" int sh_balance_loss(const sh_balance_args* args, void* stream) {
+  if (int rc = bl_check(args, false)) return rc;
+  const sh_balance_args& p = *args;
+  cudaStream_t st = (cudaStream_t)stream;
+  int sms = 0;
+  if (int rc = device_sms(&sms)) return rc;
+  const BlPlan pl = bl_plan_for(p, false, sms);
+  BlArgs a;
+  bl_fill(p, pl, a);
+  char* ws = (char*)p.workspace;
+  const size_t cols = (size_t)a.gates * a.E;
+  a.ticket = (unsigned*)ws;
+  a.part_p = (float*)(ws + kBlHead + bl_losses(a.gates));
+  a.part_n = (int*)(a.part_p + (size_t)pl.nx * cols);
+  if (int rc = bl_dispatch(p.dtype, a, pl, 0, false, st)) return rc;
+  BlOut o;
+  o.part_p = a.part_p; o.part_n = a.part_n; o.ticket = a.ticket; o.gate_loss = (double*)(ws + kBlHead);
+  o.blocks = pl.nx; o.gates = a.gates; o.E = a.E; o.kind = p.kind; o.coef = p.coef;
+  o.loss = p.loss; o.prob = p.prob; o.slope = p.slope; o.counts = p.counts;
+  return launch_k(true, sh_balance_loss_kernel, dim3((unsigned)a.gates), dim3(BL_THREADS), 0, st, o);
+}
+
+extern "C" int sh_balance_backward(const sh_balance_args* args, void* stream) {
+  if (int rc = bl_check(args, true)) return rc;
+  const sh_balance_args& p = *args;
+  if (p.n_tokens == 0) return SH_OK;
+  int sms = 0;
+  if (int rc = device_sms(&sms)) return rc;
+  const BlPlan pl = bl_plan_for(p, true, sms);
+  BlArgs a;
+  bl_fill(p, pl, a);
+  return bl_dispatch(p.dtype, a, pl, 1, false, (cudaStream_t)stream);
+}
+
+extern "C" int sh_dropout(const sh_dropout_args* args, void* stream) {
+  sh_set_error("%s", "");
+  if (!args) { sh_set_error("args is NULL"); return SH_ERR_INVALID_ARG; }
+  const sh_dropout_args& p = *args;
+  if (!dtype_ok(p.dtype, true)) return SH_ERR_INVALID_ARG;
+  if (p.rows < 0 || p.cols < 0) { sh_set_error("rows and cols must not be negative (got %lld, %lld)", (long long)p.rows, (long long)p.cols); return SH_ERR_INVALID_ARG; }
+  if (p.rows > (1ll << 32) || p.cols > (1ll << 31) - 8) {
+    sh_set_error("at most 2^32 rows and 2^31-8 cols (got %lld, %lld)", (long long)p.rows, (long long)p.cols);
+    return SH_ERR_UNSUPPORTED;
+  }
+  if (!(p.p >= 0.0 && p.p <= 1.0)) { sh_set_error("p must be in 0..1 (got %g)", p.p); return SH_ERR_INVALID_ARG; }
+  if (p.rows == 0 || p.cols == 0) return SH_OK;
+  if (!apart("y", {{p.rows, p.y_stride}})) return SH_ERR_INVALID_ARG;
+  if (!p.x || !p.y || !p.rng) { sh_set_error("x, y and rng must not be NULL"); return SH_ERR_INVALID_ARG; }
+  if ((uintptr_t)p.rng % 8) { sh_set_error("rng must be aligned to 8 bytes"); return SH_ERR_INVALID_ARG; }
+  int sms = 0;
+  if (int rc = device_sms(&sms)) return rc;
+  const size_t size = elem_bytes(p.dtype);
+  auto aligned = [&](const void* q, long long stride) { return (uintptr_t)q % 16 == 0 && (p.rows == 1 || (size_t)stride * size % 16 == 0); };
+  const bool vec = aligned(p.x, p.x_stride) && aligned(p.y, p.y_stride) && (!p.residual || aligned(p.residual, p.residual_stride));
+  DoArgs a;
+  a.x = p.x; a.residual = p.residual; a.y = p.y; a.rng = (const unsigned long long*)p.rng;
+  a.xs = p.x_stride; a.rs = p.residual_stride; a.ys = p.y_stride;
+  a.cols = (int)p.cols;
+  a.upr = (unsigned)((p.cols + 7) / 8);
+  a.limit = (int)lrint(p.p * 65536.0);
+  a.scale = a.limit < 65536 ? (float)(65536.0 / (65536 - a.limit)) : 0.f;
+  const long long most = (1ll << 31) / a.upr < 1 ? 1 : (1ll << 31) / a.upr;           // rows of a launch
+  for (long long r = 0; r < p.rows; r += most) {
+    const long long n = p.rows - r < most ? p.rows - r : most;
+    a.row0 = (unsigned)r; a.units = (unsigned)(n * a.upr);
+    const long long blocks = ((long long)a.units + DO_THREADS - 1) / DO_THREADS, cap = 16ll * sms;
+    const dim3 grid((unsigned)(blocks < cap ? blocks : cap));
+    auto go = [&](auto kern) { return launch_k(false, kern, grid, dim3(DO_THREADS), 0, (cudaStream_t)stream, a); };
+    auto typed = [&](auto zero) {
+      using T = decltype(zero);
+      if (p.residual) return vec ? go(sh_dropout_kernel<T, true, true>) : go(sh_dropout_kernel<T, false, true>);
+      return vec ? go(sh_dropout_kernel<T, true, false>) : go(sh_dropout_kernel<T, false, false>);
+    };
+    const int rc = p.dtype == SH_F32 ? typed(0.f) : p.dtype == SH_BF16 ? typed(__nv_bfloat16()) : typed(__half());
+    if (rc) return rc;
+  }
+  return SH_OK;
+}

@@ -1,0 +1,60 @@
+// Vectors of V stored values as fp32 in registers: loads, stores, conversions of the streaming kernels.
+#pragma once
+#include "sh_internal.cuh"
+
+// V values of T from p (aligned to V values) to fp32.  ONCE: what no other thread reads goes past L1.
+template <typename T, int V, bool ONCE = true>
+__device__ __forceinline__ void sh_load(const T* p, float (&f)[V]) {
+  constexpr int BYTES = V * (int)sizeof(T);
+  if constexpr (BYTES >= 4) {
+    uint32_t w[BYTES / 4];
+    if constexpr (BYTES >= 16) {
+#pragma unroll
+      for (int i = 0; i < BYTES / 16; ++i) {
+        const uint4 v = ONCE ? __ldcs(reinterpret_cast<const uint4*>(p) + i) : __ldg(reinterpret_cast<const uint4*>(p) + i);
+        w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+      }
+    } else if constexpr (BYTES == 8) {
+      const uint2 v = ONCE ? __ldcs(reinterpret_cast<const uint2*>(p)) : __ldg(reinterpret_cast<const uint2*>(p));
+      w[0] = v.x; w[1] = v.y;
+    } else {
+      w[0] = ONCE ? __ldcs(reinterpret_cast<const uint32_t*>(p)) : __ldg(reinterpret_cast<const uint32_t*>(p));
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if constexpr (sizeof(T) == 4) f[i] = __uint_as_float(w[i]);
+      else f[i] = sh_to_float<T>(reinterpret_cast<const T*>(w)[i]);
+    }
+  } else {
+    f[0] = sh_to_float<T>(p[0]);
+  }
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void sh_store(T* p, const float (&f)[V]) {
+  constexpr int BYTES = V * (int)sizeof(T);
+  if constexpr (BYTES >= 4) {
+    uint32_t w[BYTES / 4];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(f[i]);
+      else reinterpret_cast<T*>(w)[i] = sh_from_float<T>(f[i]);
+    }
+    if constexpr (BYTES >= 16) {
+#pragma unroll
+      for (int i = 0; i < BYTES / 16; ++i) reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    } else if constexpr (BYTES == 8) {
+      *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    } else {
+      *reinterpret_cast<uint32_t*>(p) = w[0];
+    }
+  } else {
+    p[0] = sh_from_float<T>(f[0]);
+  }
+}
+
+// Sum over groups of `lanes` neighbouring lanes (a power of two), the same in every lane of a group.
+__device__ __forceinline__ float sh_group_sum(float v, int lanes) {
+  for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}

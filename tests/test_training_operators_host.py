@@ -1,0 +1,106 @@
+"""Host-side checks of the training operators that need no GPU: refused arguments are refused before any CUDA call, with a
+reason; the packed arguments have the header's layout."""
+import pytest
+import torch
+
+from paper_2312_07987_b200 import binding as b
+
+HEADS = ("data", "batch_stride", "token_stride", "head_stride", "heads", "reserved")
+NORM = ("gq", "gk", "dgq", "dgk", "positions", "workspace", "workspace_bytes", "base", "dtype", "batch", "seq", "d_head", "rotated", "halves", "positions_64", "eps", "q_scale", "reserved")
+BALANCE = ("n_tokens", "token_stride", "dtoken_stride", "logits", "idx", "mask", "gloss", "loss", "prob", "slope", "counts", "dlogits", "workspace", "workspace_bytes",
+           "dtype", "kind", "sides", "n_heads", "n_experts", "k", "coef", "reserved")
+DROPOUT = ("x", "residual", "y", "rng", "rows", "cols", "x_stride", "residual_stride", "y_stride", "p", "dtype", "reserved")
+PTR = 0x1000          # never used as an address: each call below is refused
+
+
+def norm_args(heads=None, **kw):
+    h = {n: dict(data=PTR, batch_stride=256, token_stride=64, head_stride=32, heads=2, reserved=0) for n in ("q", "k", "q_out", "k_out", "dq", "dk")}
+    for n, v in (heads or {}).items():
+        h[n].update(v)
+    f = dict(gq=0, gk=0, dgq=0, dgk=0, positions=0, workspace=0, workspace_bytes=0, base=10000.0, dtype=b.SH_F32, batch=2, seq=4, d_head=32, rotated=32, halves=0,
+             positions_64=0, eps=1e-6, q_scale=1.0, reserved=0)
+    f.update(kw)
+    return b._QK_NORM.pack(*[h[n][m] for n in h for m in HEADS], *[f[n] for n in NORM])
+
+
+@pytest.mark.parametrize("kw,heads,code,frag", [
+    (dict(dtype=3), {}, -1, "dtype"), (dict(batch=-1), {}, -1, "batch"), (dict(seq=-1), {}, -1, "seq"), (dict(d_head=0), {}, -1, "d_head"),
+    (dict(d_head=257), {}, -1, "d_head"), (dict(rotated=3), {}, -1, "rotated"), (dict(rotated=34), {}, -1, "rotated"), (dict(rotated=-2), {}, -1, "rotated"),
+    (dict(d_head=33, rotated=32), {}, -2, "even d_head"), (dict(base=0.0), {}, -1, "base"), (dict(base=float("nan")), {}, -1, "base"), (dict(eps=0.0), {}, -1, "eps"),
+    (dict(eps=float("nan")), {}, -1, "eps"), (dict(q_scale=float("inf")), {}, -1, "q_scale"), ({}, dict(q=dict(heads=-1)), -1, "heads"), ({}, dict(k=dict(data=0)), -1, "k: data"),
+    ({}, dict(q_out=dict(data=0)), -1, "q_out"), ({}, dict(k_out=dict(token_stride=0)), -1, "share an address"), ({}, dict(q_out=dict(head_stride=0)), -1, "share an address"),
+])
+def test_norm_refusals(kw, heads, code, frag):
+    for fn in (b.lib.sh_qk_norm, b.lib.sh_qk_norm_backward):
+        assert fn(norm_args(heads, **kw), None) == code
+        assert frag in b.sh_last_error()
+
+
+def test_norm_backward_refusals():
+    fn = b.lib.sh_qk_norm_backward
+    assert fn(norm_args(dict(dq=dict(data=0))), None) == -1 and "dq" in b.sh_last_error()
+    assert fn(norm_args(dgq=PTR), None) == -4 and "workspace" in b.sh_last_error()
+    need = b.lib.sh_qk_norm_workspace_bytes(32)
+    assert need > 0 and b.lib.sh_qk_norm_workspace_bytes(0) == 0 and b.lib.sh_qk_norm_workspace_bytes(257) == 0
+    assert fn(norm_args(dgq=PTR, workspace=PTR + 8, workspace_bytes=need), None) == -4
+    assert fn(norm_args(dgk=PTR, workspace=PTR, workspace_bytes=need - 1), None) == -4 and "too small" in b.sh_last_error()
+    for f in (b.lib.sh_qk_norm, fn, b.lib.sh_balance_loss, b.lib.sh_balance_backward, b.lib.sh_dropout):
+        assert f(None, None) == -1 and "NULL" in b.sh_last_error()
+
+
+def test_norm_of_no_rows_needs_no_device():
+    assert b.lib.sh_qk_norm(norm_args(batch=0), None) == 0
+    assert b.lib.sh_qk_norm(norm_args(seq=0, rotated=0), None) == 0
+
+
+def balance_args(**kw):
+    f = dict(n_tokens=8, token_stride=16, dtoken_stride=16, logits=PTR, idx=PTR, mask=0, gloss=0, loss=PTR, prob=PTR, slope=PTR, counts=PTR, dlogits=PTR, workspace=PTR,
+             workspace_bytes=1 << 30, dtype=b.SH_F32, kind=0, sides=2, n_heads=2, n_experts=4, k=2, coef=1.0, reserved=0)
+    f.update(kw)
+    return b._BALANCE.pack(*[f[n] for n in BALANCE])
+
+
+@pytest.mark.parametrize("kw,code,frag", [
+    (dict(dtype=b.SH_F16), -1, "dtype"), (dict(n_tokens=-1), -1, "n_tokens"), (dict(sides=0), -1, "sides"), (dict(n_heads=0), -1, "n_heads"), (dict(n_experts=33), -1, "n_experts"),
+    (dict(sides=256, n_heads=256), -2, "65535"), (dict(logits=0), -1, "logits"), (dict(k=0), -1, "k must"), (dict(k=5), -1, "k must"), (dict(n_tokens=1 << 30), -2, "2^31"),
+    (dict(kind=2), -1, "kind"), (dict(coef=float("nan")), -1, "coef"), (dict(idx=0), -1, "idx"), (dict(loss=0), -1, "loss"), (dict(counts=0), -1, "counts"),
+    (dict(workspace=0), -4, "workspace"), (dict(workspace=PTR + 16), -4, "256"), (dict(workspace_bytes=100), -4, "too small"),
+])
+def test_balance_refusals(kw, code, frag):
+    assert b.lib.sh_balance_loss(balance_args(**kw), None) == code
+    assert frag in b.sh_last_error()
+
+
+@pytest.mark.parametrize("kw,frag", [(dict(slope=0), "slope"), (dict(dlogits=0), "dlogits"), (dict(dtoken_stride=0), "share an address"), (dict(dtype=7), "dtype"), (dict(logits=0), "logits")])
+def test_balance_backward_refusals(kw, frag):
+    assert b.lib.sh_balance_backward(balance_args(**kw), None) == -1
+    assert frag in b.sh_last_error()
+
+
+def test_balance_workspace():
+    assert b.lib.sh_balance_workspace_bytes(2, 8, 16) > b.lib.sh_balance_workspace_bytes(2, 2, 4) > 0
+    assert b.lib.sh_balance_workspace_bytes(0, 8, 16) == 0 and b.lib.sh_balance_workspace_bytes(1, 1, 33) == 0
+
+
+@pytest.mark.parametrize("kw,code,frag", [
+    (dict(dtype=5), -1, "dtype"), (dict(rows=-1), -1, "rows"), (dict(cols=-1), -1, "cols"), (dict(cols=1 << 31), -2, "cols"), (dict(rows=(1 << 32) + 1), -2, "rows"), (dict(p=-0.1), -1, "p must"),
+    (dict(p=1.5), -1, "p must"), (dict(p=float("nan")), -1, "p must"), (dict(x=0), -1, "x, y"), (dict(y=0), -1, "x, y"), (dict(rng=0), -1, "rng"), (dict(rng=PTR + 4), -1, "rng"),
+    (dict(y_stride=0), -1, "share an address"),
+])
+def test_dropout_refusals(kw, code, frag):
+    f = dict(x=PTR, residual=0, y=PTR, rng=PTR, rows=4, cols=64, x_stride=64, residual_stride=64, y_stride=64, p=0.1, dtype=b.SH_F32, reserved=0)
+    f.update(kw)
+    assert b.lib.sh_dropout(b._DROPOUT.pack(*[f[n] for n in DROPOUT]), None) == code
+    assert frag in b.sh_last_error()
+
+
+def test_binding_refuses_host_tensors():
+    x = torch.zeros(2, 4, 2, 32)
+    with pytest.raises(ValueError, match="CUDA"):
+        b.sh_qk_norm(x, x)
+    with pytest.raises(ValueError, match="CUDA"):
+        b.sh_balance_loss(x, torch.zeros(4, 2, 2, 2, dtype=torch.int32))
+    with pytest.raises(ValueError, match="CUDA"):
+        b.sh_balance_backward(x, x)
+    with pytest.raises(ValueError, match="CUDA"):
+        b.sh_dropout(x, torch.zeros(2, dtype=torch.int64), 0.1)
