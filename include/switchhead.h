@@ -282,7 +282,6 @@ int sh_backward(sh_layer* layer, const void* x, const float* dout, float* dx, fl
 typedef struct {
   void* data;
   int64_t batch_stride, token_stride, head_stride;
-  int32_t heads, reserved;
 } sh_heads;
 
 /* Norms of queries and keys for each head, with the position rotation in the same pass.  For every row x of d_head values
@@ -290,32 +289,38 @@ typedef struct {
  *   n = g o x / sqrt(mean(x^2) + eps),   y = Rot(position) n   (queries: times q_scale)
  * Rot turns the pair i < rotated/2 of the first `rotated` columns by position * base^(-2i/rotated): the columns (2i, 2i+1), as
  * sh_set_rope does, or with halves != 0 the columns (i, i + rotated/2).  rotated = 0: no rotation.  Statistics in fp32, one rounding to
- * the stored type.  Angles are exact to 2^-24 turns at every position a 32-bit integer holds.
+ * the stored type.  Angles are good to 2^-24 turns at every position a 32-bit integer holds (16-bit types: and sine and cosine
+ * to 2^-21).
  *   dtype      of q, k, their outputs and gradients: SH_F32, SH_BF16 or SH_F16
- *   q, k       heads may be 0 (that side is left out), and need not be equal (grouped heads)
- *   q_out, k_out   the normalised and rotated heads (sh_qk_norm), or the gradients of q and k (sh_qk_norm_backward); their
- *              `heads` is ignored.  May be q and k themselves (same strides), or dq and dk; otherwise no overlap.
+ *   q, k       q_heads, k_heads may be 0 (that side is left out), and need not be equal (grouped heads)
+ *   q_out, k_out   the normalised and rotated heads (sh_qk_norm), or the gradients of q and k (sh_qk_norm_backward).  May be
+ *              q and k themselves (same strides), or dq and dk; otherwise no overlap.
  *   gq, gk     [d_head] fp32 gains, shared by a side's heads; NULL: ones
  *   positions  [batch, seq] int32 (positions_64 != 0: int64), any values; NULL: token t of a sequence is at position t
- *   d_head 1..256, even with a rotation; eps positive.
- * Backward (q, k: the inputs of the forward call; dq, dk: the gradients of its outputs): writes the gradients of q and k to
- * q_out, k_out and those of the gains, summed over tokens and heads, to dgq, dgk [d_head] fp32 (NULL: not wanted; a sum over no
- * rows is zero).  The workspace, sh_qk_norm_workspace_bytes(d_head) bytes aligned to 256, is wanted with dgq or dgk.
- * The same inputs give the same bits. */
+ *   d_head 1..256, even with a rotation; eps positive. */
 typedef struct {
-  sh_heads q, k, q_out, k_out, dq, dk;
+  sh_heads q, k, q_out, k_out;
   const float *gq, *gk;
-  float *dgq, *dgk;
   const void* positions;
-  void* workspace;
-  size_t workspace_bytes;
   double base;
-  int32_t dtype, batch, seq, d_head, rotated, halves, positions_64;
+  int32_t dtype, batch, seq, q_heads, k_heads, d_head, rotated, halves, positions_64;
   float eps, q_scale;
   int32_t reserved;
 } sh_qk_norm_args;
 int sh_qk_norm(const sh_qk_norm_args* args, void* stream);
-int sh_qk_norm_backward(const sh_qk_norm_args* args, void* stream);
+
+/* Its gradients: norm.q, norm.k are the inputs of the forward call, dq, dk the gradients of its outputs.  Writes the gradients
+ * of q and k to norm.q_out, norm.k_out and those of the gains, summed over tokens and heads, to dgq, dgk [d_head] fp32 (NULL: not
+ * wanted; a sum over no rows is zero).  The workspace, sh_qk_norm_workspace_bytes(d_head) bytes aligned to 256, is wanted with
+ * dgq or dgk.  The same inputs give the same bits. */
+typedef struct {
+  sh_qk_norm_args norm;
+  sh_heads dq, dk;
+  float *dgq, *dgk;
+  void* workspace;
+  size_t workspace_bytes;
+} sh_qk_norm_backward_args;
+int sh_qk_norm_backward(const sh_qk_norm_backward_args* args, void* stream);
 size_t sh_qk_norm_workspace_bytes(int d_head);
 
 /* Balance loss of the gates, with the per-expert counts.  logits [N, sides, H, E] fp32 or bf16 (a token's gates dense, tokens

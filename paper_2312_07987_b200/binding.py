@@ -302,68 +302,80 @@ def sh_noalloc_gate_topk(dtype: int, x: torch.Tensor, w_gate: torch.Tensor, bias
     return idx, gate, offsets, lists
 
 
-# The operators of a training step (switchhead.h).  Their arguments are one C struct, packed here field by field.
-_HEADS = "P3q2i"
-_QK_NORM = struct.Struct(_HEADS * 6 + "6PQd7i2fi")
+# The operators of a training step (switchhead.h).  Their arguments are one C struct, packed here field by field: small calls
+# are bound by what happens on the host.
+_QK_NORM_FIELDS = "P3q" * 4 + "3Pd9i2fi"
+_QK_NORM = struct.Struct(_QK_NORM_FIELDS)
+_QK_NORM_BACKWARD = struct.Struct(_QK_NORM_FIELDS + "P3q" * 2 + "3PQ")
 _BALANCE = struct.Struct("3q10PQ6ifi")
 _DROPOUT = struct.Struct("4P5qd2i")
 _DTYPES = {torch.float32: SH_F32, torch.bfloat16: SH_BF16, torch.float16: SH_F16}
+_NO_HEADS = (0, 0, 0, 0)
 
 
-def _launch(fn, packed: bytes, device: torch.device) -> None:
+def _launch(fn, packed: bytes, device: int) -> None:
     """The call on the tensors' device and on the stream that is current there."""
-    if device.index == torch.cuda.current_device():
-        _check(fn(packed, torch.cuda.current_stream(device).cuda_stream))
+    if device == torch.cuda.current_device():
+        rc = fn(packed, torch._C._cuda_getCurrentRawStream(device))     # (torch.cuda.current_stream makes an object first: 2 us of a 10 us call)
     else:
         with torch.cuda.device(device):
-            _check(fn(packed, torch.cuda.current_stream(device).cuda_stream))
+            rc = fn(packed, torch._C._cuda_getCurrentRawStream(device))
+    if rc != SH_OK:
+        raise SwitchHeadError(rc)
 
 
-def _refuse_unless(ok: bool, message: str) -> None:
-    if not ok:
-        raise ValueError(message)
+def _strides(t: torch.Tensor) -> tuple:
+    s = t.stride()
+    return t.data_ptr(), s[0], s[1], s[2]
 
 
-def _heads(name: str, t: Optional[torch.Tensor], like: torch.Tensor, shape) -> tuple:
+def _heads(name: str, t: torch.Tensor, like: torch.Tensor, shape) -> tuple:
     """The fields of one sh_heads: t [B, T, heads, d_head], the last dimension dense."""
-    if t is None:
-        return (0, 0, 0, 0, 0, 0)
-    st = t.stride()
-    if t.shape != shape or t.dtype != like.dtype or t.device != like.device or (st[3] != 1 and shape[3] > 1):
+    s = t.stride()
+    if t.shape != shape or t.dtype != like.dtype or t.get_device() != like.get_device() or (s[3] != 1 and shape[3] > 1):
         raise ValueError(f"{name} must be [batch, seq, heads, d_head] = {tuple(shape)} of {like.dtype} on {like.device}, its last dimension "
-                         f"dense: got {tuple(t.shape)}, {t.dtype}, {t.device}, strides {tuple(st)}")
-    return (t.data_ptr(), st[0], st[1], st[2], shape[2], 0)
+                         f"dense: got {tuple(t.shape)}, {t.dtype}, {t.device}, strides {tuple(s)}")
+    return t.data_ptr(), s[0], s[1], s[2]
 
 
 def _dense_f32(name: str, t: Optional[torch.Tensor], like: torch.Tensor, shape) -> int:
     if t is None:
         return 0
-    if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or t.device != like.device or not t.is_contiguous():
+    if t.dtype != torch.float32 or t.shape != shape or t.get_device() != like.get_device() or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous fp32 tensor {tuple(shape)} on {like.device}: got {tuple(t.shape)}, {t.dtype}, {t.device}")
     return t.data_ptr()
 
 
-def _qk_norm_pack(q, k, q_out, k_out, dq, dk, gq, gk, dgq, dgk, workspace, eps, base, rotated, halves, positions, q_scale) -> bytes:
-    shape = q.shape
+def _qk_norm_fields(q, k, q_out, k_out, gq, gk, eps, base, rotated, halves, positions, q_scale) -> tuple:
+    """The fields of sh_qk_norm_args.  An output that is None is made here; returns (fields, q_out, k_out)."""
     if q.dim() != 4 or q.dtype not in _DTYPES or not q.is_cuda:
-        raise ValueError(f"q must be a CUDA tensor [batch, seq, heads, d_head] of fp32, bf16 or fp16: got {tuple(shape)}, {q.dtype}, {q.device}")
-    ks = None
+        raise ValueError(f"q must be a CUDA tensor [batch, seq, heads, d_head] of fp32, bf16 or fp16: got {tuple(q.shape)}, {q.dtype}, {q.device}")
+    shape = q.shape
+    B, T, H, D = shape
+    hq = _heads("q", q, q, shape)
+    if q_out is None:
+        q_out = torch.empty_like(q)
+        oq = _strides(q_out)
+    else:
+        oq = _heads("the output for q", q_out, q, shape)
+    hk, ok, K = _NO_HEADS, _NO_HEADS, 0
     if k is not None:
         ks = k.shape
-        if k.dim() != 4 or ks[0] != shape[0] or ks[1] != shape[1] or ks[3] != shape[3]:
-            raise ValueError(f"k must be [batch, seq, heads, d_head] with q's batch, seq and d_head: got {tuple(ks)}, q {tuple(shape)}")
-    pos = 0
+        K = ks[2] if len(ks) == 4 else 0
+        hk = _heads("k", k, q, (B, T, K, D))
+        if k_out is None:
+            k_out = torch.empty_like(k)
+            ok = _strides(k_out)
+        else:
+            ok = _heads("the output for k", k_out, q, ks)
+    pos = wide = 0
     if positions is not None:
-        if positions.shape != shape[:2] or positions.dtype not in (torch.int32, torch.int64) or positions.device != q.device or not positions.is_contiguous():
-            raise ValueError(f"positions must be a contiguous int32 or int64 tensor {tuple(shape[:2])} on {q.device}: got {tuple(positions.shape)}, {positions.dtype}, {positions.device}")
+        wide = positions.dtype == torch.int64
+        if positions.shape != (B, T) or not (wide or positions.dtype == torch.int32) or positions.get_device() != q.get_device() or not positions.is_contiguous():
+            raise ValueError(f"positions must be a contiguous int32 or int64 tensor {(B, T)} on {q.device}: got {tuple(positions.shape)}, {positions.dtype}, {positions.device}")
         pos = positions.data_ptr()
-    D = shape[3]
-    one = (D,)
-    return _QK_NORM.pack(*_heads("q", q, q, shape), *_heads("k", k, q, ks), *_heads("the output for q", q_out, q, shape), *_heads("the output for k", k_out, q, ks),
-                         *_heads("dq", dq, q, shape), *_heads("dk", dk, q, ks), _dense_f32("gq", gq, q, one), _dense_f32("gk", gk, q, one),
-                         0 if dgq is None else dgq.data_ptr(), 0 if dgk is None else dgk.data_ptr(), pos,
-                         0 if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(), base,
-                         _DTYPES[q.dtype], shape[0], shape[1], D, rotated, 1 if halves else 0, 1 if pos and positions.dtype == torch.int64 else 0, eps, q_scale, 0)
+    return (*hq, *hk, *oq, *ok, _dense_f32("gq", gq, q, (D,)), _dense_f32("gk", gk, q, (D,)), pos, base,
+            _DTYPES[q.dtype], B, T, H, K, D, rotated, halves, wide, eps, q_scale, 0), q_out, k_out
 
 
 def sh_qk_norm(q: torch.Tensor, k: Optional[torch.Tensor], gq: Optional[torch.Tensor] = None, gk: Optional[torch.Tensor] = None, *, eps: float = 1e-6,
@@ -372,11 +384,8 @@ def sh_qk_norm(q: torch.Tensor, k: Optional[torch.Tensor], gq: Optional[torch.Te
     """Queries and keys normalised per head and rotated by their position, in one pass.  q, k [batch, seq, heads, d_head] in any strides
     with a dense last dimension (columns of a fused projection, transposed views); k may be None.  gq, gk [d_head] fp32 gains.
     q_out, k_out: where the results go (q and k themselves are allowed).  Returns (q_out, k_out)."""
-    if q_out is None:
-        q_out = torch.empty_like(q)
-    if k_out is None and k is not None:
-        k_out = torch.empty_like(k)
-    _launch(lib.sh_qk_norm, _qk_norm_pack(q, k, q_out, k_out, None, None, gq, gk, None, None, None, eps, base, rotated, halves, positions, q_scale), q.device)
+    fields, q_out, k_out = _qk_norm_fields(q, k, q_out, k_out, gq, gk, eps, base, rotated, halves, positions, q_scale)
+    _launch(lib.sh_qk_norm, _QK_NORM.pack(*fields), q.get_device())
     return q_out, k_out
 
 
@@ -390,18 +399,32 @@ def _balance_workspace_bytes(sides: int, heads: int, experts: int) -> int:
     return lib.sh_balance_workspace_bytes(sides, heads, experts)
 
 
+def _dense(shape: tuple, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
+    """torch.empty (empty_strided skips 1 us of it)."""
+    strides, n = [], 1
+    for s in reversed(shape):
+        strides.append(n)
+        n *= s if s > 1 else 1
+    return torch.empty_strided(shape, strides[::-1], dtype=dtype, device=device)
+
+
 def sh_qk_norm_backward(q: torch.Tensor, k: Optional[torch.Tensor], dq: torch.Tensor, dk: Optional[torch.Tensor], gq: Optional[torch.Tensor] = None,
                         gk: Optional[torch.Tensor] = None, *, eps: float = 1e-6, base: float = 10000.0, rotated: int = 0, halves: bool = False,
                         positions: Optional[torch.Tensor] = None, q_scale: float = 1.0) -> dict:
     """Gradients of sh_qk_norm(q, k, gq, gk, ...) from those of its outputs, dq and dk: {dq, dk} with respect to its inputs, and of the
     gains that were given (dgq, dgk [d_head] fp32, summed over tokens and heads; None where there is no gain)."""
-    _refuse_unless(dq is not None and (dk is None) == (k is None), "dq and, with k, dk must be given")
-    out_q, out_k = torch.empty_like(q), None if k is None else torch.empty_like(k)
-    D = q.shape[-1]
-    dgq = None if gq is None else torch.empty(D, dtype=torch.float32, device=q.device)
-    dgk = None if gk is None else torch.empty(D, dtype=torch.float32, device=q.device)
-    ws = None if gq is None and gk is None else torch.empty(_qk_norm_workspace_bytes(D), dtype=torch.uint8, device=q.device)
-    _launch(lib.sh_qk_norm_backward, _qk_norm_pack(q, k, out_q, out_k, dq, dk, gq, gk, dgq, dgk, ws, eps, base, rotated, halves, positions, q_scale), q.device)
+    if dq is None or (dk is None) != (k is None):
+        raise ValueError("dq and, with k, dk must be given")
+    fields, out_q, out_k = _qk_norm_fields(q, k, None, None, gq, gk, eps, base, rotated, halves, positions, q_scale)
+    dgq = None if gq is None else torch.empty_like(gq)
+    dgk = None if gk is None else torch.empty_like(gk)
+    ws, nbytes = None, 0
+    if gq is not None or gk is not None:
+        nbytes = _qk_norm_workspace_bytes(q.shape[3])
+        ws = _dense((nbytes,), torch.uint8, q.device)
+    _launch(lib.sh_qk_norm_backward, _QK_NORM_BACKWARD.pack(*fields, *_heads("dq", dq, q, q.shape), *(_NO_HEADS if k is None else _heads("dk", dk, q, k.shape)),
+                                                            0 if dgq is None else dgq.data_ptr(), 0 if dgk is None else dgk.data_ptr(),
+                                                            0 if ws is None else ws.data_ptr(), nbytes), q.get_device())
     return dict(dq=out_q, dk=out_k, dgq=dgq, dgk=dgk)
 
 
@@ -416,7 +439,7 @@ def _logits(name: str, z: torch.Tensor) -> None:
 def _token_mask(mask: Optional[torch.Tensor], z: torch.Tensor) -> int:
     if mask is None:
         return 0
-    if mask.dtype not in (torch.bool, torch.uint8) or mask.shape != z.shape[:1] or mask.device != z.device or not mask.is_contiguous():
+    if mask.dtype not in (torch.bool, torch.uint8) or mask.shape != z.shape[:1] or mask.get_device() != z.get_device() or not mask.is_contiguous():
         raise ValueError(f"mask must be a contiguous bool or uint8 tensor [{z.shape[0]}] on {z.device}: got {tuple(mask.shape)}, {mask.dtype}, {mask.device}")
     return mask.data_ptr()
 
@@ -427,20 +450,20 @@ def sh_balance_loss(logits: torch.Tensor, idx: torch.Tensor, *, kind: str = "cou
     [sides, heads, experts]; slope is what sh_balance_backward takes."""
     _logits("logits", logits)
     N, S, H, E = logits.shape
-    if idx.dtype != torch.int32 or idx.dim() != 4 or idx.shape[:3] != (S, N, H) or idx.device != logits.device or not idx.is_contiguous():
+    if idx.dtype != torch.int32 or idx.dim() != 4 or idx.shape[:3] != (S, N, H) or idx.get_device() != logits.get_device() or not idx.is_contiguous():
         raise ValueError(f"idx must be a contiguous int32 tensor [sides, tokens, heads, k] on {logits.device}: got {tuple(idx.shape)}, {idx.dtype}, {idx.device}")
     if kind not in SH_BALANCE:
         raise ValueError(f"kind must be one of {sorted(SH_BALANCE)}: got {kind!r}")
     dev = logits.device
-    loss = torch.empty((), dtype=torch.float32, device=dev)
-    prob = torch.empty((S, H, E), dtype=torch.float32, device=dev)
-    slope = torch.empty((S, H, E), dtype=torch.float32, device=dev)
-    counts = torch.empty((S, H, E), dtype=torch.int32, device=dev)
+    loss = _dense((), torch.float32, dev)
+    prob = _dense((S, H, E), torch.float32, dev)
+    slope = torch.empty_like(prob)
+    counts = torch.empty_like(prob, dtype=torch.int32)
     nbytes = _balance_workspace_bytes(S, H, E)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    ws = _dense((nbytes,), torch.uint8, dev)
     _launch(lib.sh_balance_loss, _BALANCE.pack(N, logits.stride(0), 0, logits.data_ptr(), idx.data_ptr(), _token_mask(mask, logits), 0, loss.data_ptr(),
                                                prob.data_ptr(), slope.data_ptr(), counts.data_ptr(), 0, ws.data_ptr(), nbytes,
-                                               _DTYPES[logits.dtype], SH_BALANCE[kind], S, H, E, idx.shape[3], coef, 0), dev)
+                                               _DTYPES[logits.dtype], SH_BALANCE[kind], S, H, E, idx.shape[3], coef, 0), logits.get_device())
     return dict(loss=loss, counts=counts, prob=prob, slope=slope)
 
 
@@ -451,16 +474,26 @@ def sh_balance_backward(logits: torch.Tensor, slope: torch.Tensor, *, gloss: Opt
     _logits("logits", logits)
     N, S, H, E = logits.shape
     if out is None:
-        out = torch.empty((N, S, H, E), dtype=logits.dtype, device=logits.device)
-    elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device:
+        out = torch.empty_like(logits, memory_format=torch.contiguous_format)
+    elif out.shape != logits.shape or out.dtype != logits.dtype or out.get_device() != logits.get_device():
         raise ValueError("out must have the shape, type and device of logits")
     else:
         _logits("out", out)
     _launch(lib.sh_balance_backward, _BALANCE.pack(N, logits.stride(0), out.stride(0), logits.data_ptr(), 0, _token_mask(mask, logits),
-                                                   _dense_f32("gloss", gloss, logits, ()),
-                                                   0, 0, _dense_f32("slope", slope, logits, (S, H, E)), 0, out.data_ptr(), 0, 0,
-                                                   _DTYPES[logits.dtype], 0, S, H, E, 1, 0.0, 0), logits.device)
+                                                   _dense_f32("gloss", gloss, logits, ()), 0, 0, _dense_f32("slope", slope, logits, (S, H, E)), 0,
+                                                   out.data_ptr(), 0, 0, _DTYPES[logits.dtype], 0, S, H, E, 1, 0.0, 0), logits.get_device())
     return out
+
+
+def _rows(name: str, t: torch.Tensor, x: torch.Tensor) -> int:
+    """The row stride of a matrix of x's shape (leading dimensions flattened)."""
+    if t.shape != x.shape or t.dtype != x.dtype or t.get_device() != x.get_device():
+        raise ValueError(f"{name} must have the shape, type and device of x")
+    if t.is_contiguous():
+        return t.shape[-1]
+    if t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1):
+        return t.stride(0)
+    raise ValueError(f"{name} must be contiguous, or a matrix with dense rows")
 
 
 def sh_dropout(x: torch.Tensor, rng: torch.Tensor, p: float, *, residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -469,26 +502,14 @@ def sh_dropout(x: torch.Tensor, rng: torch.Tensor, p: float, *, residual: Option
     out may be x or residual."""
     if x.dtype not in _DTYPES or not x.is_cuda or x.dim() < 1:
         raise ValueError(f"x must be a CUDA tensor [..., columns] of fp32, bf16 or fp16: got {tuple(x.shape)}, {x.dtype}, {x.device}")
-    if rng.dtype != torch.int64 or tuple(rng.shape) != (2,) or rng.device != x.device or not rng.is_contiguous():
+    if rng.dtype != torch.int64 or rng.shape != (2,) or rng.get_device() != x.get_device() or not rng.is_contiguous():
         raise ValueError(f"rng must be a contiguous int64 tensor [2] on {x.device}: got {tuple(rng.shape)}, {rng.dtype}, {rng.device}")
     if out is None:
         out = torch.empty_like(x, memory_format=torch.contiguous_format)
     cols = x.shape[-1]
-    rows = x.numel() // cols if cols else 0
-
-    def stride(name, t):
-        if t.shape != x.shape or t.dtype != x.dtype or t.device != x.device:
-            raise ValueError(f"{name} must have the shape, type and device of x")
-        if t.is_contiguous():
-            return cols
-        if t.dim() == 2 and (t.stride(1) == 1 or cols == 1):
-            return t.stride(0)
-        raise ValueError(f"{name} must be contiguous, or a matrix with dense rows")
-
-    xs, ys = stride("x", x), stride("out", out)
-    rs = 0 if residual is None else stride("residual", residual)
     _launch(lib.sh_dropout, _DROPOUT.pack(x.data_ptr(), 0 if residual is None else residual.data_ptr(), out.data_ptr(), rng.data_ptr(),
-                                          rows, cols, xs, rs, ys, p, _DTYPES[x.dtype], 0), x.device)
+                                          x.numel() // cols if cols else 0, cols, _rows("x", x, x), 0 if residual is None else _rows("residual", residual, x),
+                                          _rows("out", out, x), p, _DTYPES[x.dtype], 0), x.get_device())
     return out
 
 

@@ -10,7 +10,8 @@
 #include "sh_vec.cuh"
 
 constexpr int BL_THREADS = 256;
-constexpr int BL_MAX_BLOCKS = 592;         // blocks of the first kernel at most (rows of partial results)
+constexpr int BL_LOSS_THREADS = 512;
+constexpr int BL_MAX_BLOCKS = 512;         // blocks of the first kernel at most (rows of partial results)
 
 struct BlArgs {
   const void* z; void* dz;
@@ -24,55 +25,79 @@ struct BlArgs {
   unsigned* ticket;                        // gates whose sums are done (set to zero by the first kernel)
 };
 
-// The lane's W logits of a row.  VEC: E = L W, aligned.
+// Rows of a thread that are on their way together: 64 bytes of them.
+template <typename T, int W> struct BlAhead { static constexpr int N = W * (int)sizeof(T) >= 32 ? 2 : 4; };
+
+// The lane's W logits of a row, -inf where there are none.  VEC: E = L W, aligned.
 template <typename T, int W, bool VEC>
-__device__ __forceinline__ void bl_load(const T* p, int at, int E, float (&f)[W], float none) {
-  if constexpr (VEC) {
-    sh_load<T, W>(p + at, f);
-  } else {
+struct BlRow {
+  ShRaw<T, VEC ? W : 1> raw[VEC ? 1 : W];
+  __device__ __forceinline__ void load(const T* p, int n, bool live) {       // n: logits from p on
+    constexpr uint32_t none = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;      // -inf (two of them)
+    if constexpr (VEC) {
+      if (live) raw[0].load(p);
+      else raw[0].fill(none);
+    } else {
 #pragma unroll
-    for (int i = 0; i < W; ++i) f[i] = at + i < E ? sh_to_float<T>(p[at + i]) : none;
+      for (int i = 0; i < W; ++i) {
+        if (live && i < n) raw[i].load(p + i);
+        else raw[i].fill(none);
+      }
+    }
   }
+  __device__ __forceinline__ void get(float2 (&f)[W / 2]) const {
+    float g[W];
+    if constexpr (VEC) {
+      raw[0].get(g);
+    } else {
+#pragma unroll
+      for (int i = 0; i < W; ++i) { float one[1]; raw[i].get(one); g[i] = one[0]; }
+    }
+#pragma unroll
+    for (int i = 0; i < W / 2; ++i) f[i] = make_float2(g[2 * i], g[2 * i + 1]);
+  }
+};
+
+__device__ __forceinline__ float bl_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
-template <int L> __device__ __forceinline__ float bl_max(float v) {
-#pragma unroll
-  for (int o = L / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
-}
-template <int L> __device__ __forceinline__ float bl_sum(float v) {
-#pragma unroll
-  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-
-// p from a row's logits, in place.  A row of -inf only has no probabilities: zeros.
+// exp(z - max) of a row in place of its logits; returns 1 / their sum.  (The difference first: logits may be as large as
+// their type allows.)  A row of -inf only has no probabilities: zeros.
 template <int W, int L>
-__device__ __forceinline__ void bl_softmax(float (&f)[W]) {
-  float m = f[0];
+__device__ __forceinline__ float bl_softmax(float2 (&f)[W / 2]) {
+  float m = fmaxf(f[0].x, f[0].y);
 #pragma unroll
-  for (int i = 1; i < W; ++i) m = fmaxf(m, f[i]);
-  m = bl_max<L>(m);
-  const bool none = m == -INFINITY;                      // (a NaN is no maximum: it comes out of the exponential)
-  float s = 0.f;
+  for (int i = 1; i < W / 2; ++i) m = fmaxf(m, fmaxf(f[i].x, f[i].y));
 #pragma unroll
-  for (int i = 0; i < W; ++i) { f[i] = __isnanf(f[i]) || !none ? expf(f[i] - m) : 0.f; s += f[i]; }
-  s = bl_sum<L>(s);
-  const float inv = s == 0.f ? 0.f : 1.f / s;
+  for (int o = L / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const float log2e = 1.4426950408889634f, b = m == -INFINITY ? 0.f : -m;
+  const float2 s2 = make_float2(log2e, log2e), b2 = make_float2(b, b);
+  float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-  for (int i = 0; i < W; ++i) f[i] *= inv;
+  for (int i = 0; i < W / 2; ++i) {
+    const float2 x = __fmul2_rn(__fadd2_rn(f[i], b2), s2);
+    f[i] = make_float2(bl_exp2(x.x), bl_exp2(x.y));
+    sum = __fadd2_rn(sum, f[i]);
+  }
+  float s = sum.x + sum.y;
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return s == 0.f ? 0.f : __fdividef(1.f, s);
 }
 
 // A block's share of the sums: tokens tpb at a time, blockIdx.y's gates.
 template <typename T, int W, int L, bool VEC>
-static __global__ void __launch_bounds__(BL_THREADS) sh_balance_sums_kernel(const BlArgs a) {
-  constexpr int EP = W * L, ROWS = BL_THREADS / L;
+static __global__ void __launch_bounds__(BL_THREADS, 3) sh_balance_sums_kernel(const BlArgs a) {
+  constexpr int EP = W * L, ROWS = BL_THREADS / L, AHEAD = BlAhead<T, W>::N, PICKS = 4 / L < 1 ? 1 : 4 / L;
   __shared__ float s_p[ROWS][EP + 1];
   __shared__ int s_n[ROWS * EP];                         // [gate of the block][expert]
   __shared__ int s_tokens;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int row = threadIdx.x / L, at = (threadIdx.x % L) * W;
+  const int row = threadIdx.x / L, sub = threadIdx.x % L, at = sub * W;
   const int g0 = blockIdx.y * a.per, ng = min(a.per, a.gates - g0);
   const int gl = row % a.per, tl = row / a.per, gate = g0 + gl;
   const bool mine = tl < a.tpb && gl < ng;
@@ -80,39 +105,50 @@ static __global__ void __launch_bounds__(BL_THREADS) sh_balance_sums_kernel(cons
   if (threadIdx.x == 0) s_tokens = 0;
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.ticket = 0;
   __syncthreads();
-  float acc[W];
+  float2 acc[W / 2];
+#pragma unroll
+  for (int i = 0; i < W / 2; ++i) acc[i] = make_float2(0.f, 0.f);
   int seen = 0;
+  auto count = [&](int e) { if ((unsigned)e < (unsigned)a.E) atomicAdd(&s_n[gl * EP + e], 1); };   // (a slot without an expert is not counted)
+  const long long step = (long long)gridDim.x * a.tpb;
+  long long t = (long long)blockIdx.x * a.tpb + tl;      // (what is past the last token is not read)
+  const T* z = (const T*)a.z + (long long)gate * a.E + at + t * a.zt;
+  const int* idx = a.idx + ((long long)(gate / a.H) * a.tokens * a.H + gate % a.H + t * a.H) * a.k;
+  const long long zstep = step * a.zt, istep = step * a.H * a.k, rounds = (a.tokens - (long long)blockIdx.x * a.tpb + step - 1) / step;
+  for (long long r = 0; r < rounds; r += AHEAD) {
+    BlRow<T, W, VEC> rows[AHEAD];
+    int picks[AHEAD][PICKS];
 #pragma unroll
-  for (int i = 0; i < W; ++i) acc[i] = 0.f;
-  const T* z = (const T*)a.z + (long long)gate * a.E;
-  const int* idx = a.idx + ((long long)(gate / a.H) * a.tokens * a.H + gate % a.H) * a.k;
-  for (long long t0 = (long long)blockIdx.x * a.tpb; t0 < a.tokens; t0 += (long long)gridDim.x * a.tpb) {
-    const long long t = t0 + tl;
-    const bool live = mine && t < a.tokens && (!a.mask || a.mask[t]);
-    float f[W];
+    for (int u = 0; u < AHEAD; ++u) {
+      const bool live = mine && t < a.tokens && (!a.mask || a.mask[t]);
+      rows[u].load(z, a.E - at, live);
 #pragma unroll
-    for (int i = 0; i < W; ++i) f[i] = -INFINITY;
-    if (live) bl_load<T, W, VEC>(z + t * a.zt, at, a.E, f, -INFINITY);
-    if (live) {
-      for (int j = threadIdx.x % L; j < a.k; j += L) {
-        const unsigned e = (unsigned)idx[t * a.H * a.k + j];
-        if (e < (unsigned)a.E) atomicAdd(&s_n[gl * EP + e], 1);     // (a slot without an expert is not counted)
-      }
+      for (int j = 0; j < PICKS; ++j) picks[u][j] = live && sub * PICKS + j < a.k ? __ldcs(idx + sub * PICKS + j) : -1;
+      if (live)
+        for (int j = L * PICKS + sub; j < a.k; j += L) count(__ldcs(idx + j));
+      seen += live;
+      t += step; z += zstep; idx += istep;
     }
-    bl_softmax<W, L>(f);
 #pragma unroll
-    for (int i = 0; i < W; ++i) acc[i] += f[i];
-    seen += live;
+    for (int u = 0; u < AHEAD; ++u) {
+#pragma unroll
+      for (int j = 0; j < PICKS; ++j) count(picks[u][j]);
+      float2 f[W / 2];
+      rows[u].get(f);
+      const float inv = bl_softmax<W, L>(f);
+#pragma unroll
+      for (int i = 0; i < W / 2; ++i) acc[i] = __ffma2_rn(f[i], make_float2(inv, inv), acc[i]);
+    }
   }
-  if (mine && gl == 0 && threadIdx.x % L == 0 && seen) atomicAdd(&s_tokens, seen);
+  if (mine && gl == 0 && sub == 0 && seen) atomicAdd(&s_tokens, seen);
 #pragma unroll
-  for (int i = 0; i < W; ++i) s_p[row][at + i] = acc[i];
+  for (int i = 0; i < W / 2; ++i) { s_p[row][at + 2 * i] = acc[i].x; s_p[row][at + 2 * i + 1] = acc[i].y; }
   __syncthreads();
   const long long base = (long long)blockIdx.x * a.gates * a.E;
   for (int i = threadIdx.x; i < ng * a.E; i += BL_THREADS) {
     const int q = i / a.E, e = i % a.E;
     float sum = 0.f;
-    for (int r = 0; r < a.tpb; ++r) sum += s_p[r * a.per + q][e];
+    for (int k = 0; k < a.tpb; ++k) sum += s_p[k * a.per + q][e];
     a.part_p[base + (long long)(g0 + q) * a.E + e] = sum;
     a.part_n[base + (long long)(g0 + q) * a.E + e] = s_n[q * EP + e];
   }
@@ -128,27 +164,28 @@ struct BlOut {
 
 // A gate per block: its experts' sums over the first kernel's blocks in a fixed order, in 64 bits, its share of the loss
 // and the centred slope; the block that comes last adds the gates' losses in order.
-static __global__ void __launch_bounds__(BL_THREADS) sh_balance_loss_kernel(const BlOut a) {
-  __shared__ double s_p[BL_THREADS];
-  __shared__ int s_n[BL_THREADS], s_last;
-  __shared__ int s_t[BL_THREADS / 32];
+static __global__ void __launch_bounds__(BL_LOSS_THREADS) sh_balance_loss_kernel(const BlOut a) {
+  constexpr int ROWS = BL_LOSS_THREADS / 32;
+  __shared__ double s_p[ROWS][32];
+  __shared__ int s_n[ROWS][32], s_t[ROWS], s_last;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int gate = blockIdx.x, e = threadIdx.x & 31, r = threadIdx.x >> 5, cols = a.gates * a.E;
   double p = 0.0;
   int n = 0, tokens = 0;
   if (e < a.E)
-    for (int b = r; b < a.blocks; b += BL_THREADS / 32) {
+#pragma unroll 16
+    for (int b = r; b < a.blocks; b += ROWS) {
       p += (double)__ldcg(a.part_p + (long long)b * cols + gate * a.E + e);
       n += __ldcg(a.part_n + (long long)b * cols + gate * a.E + e);
     }
-  for (int b = threadIdx.x; b < a.blocks; b += BL_THREADS) tokens += __ldcg(a.part_n + (long long)a.blocks * cols + b);
-  s_p[threadIdx.x] = p; s_n[threadIdx.x] = n;
+  for (int b = threadIdx.x; b < a.blocks; b += BL_LOSS_THREADS) tokens += __ldcg(a.part_n + (long long)a.blocks * cols + b);
+  s_p[r][e] = p; s_n[r][e] = n;
   for (int o = 16; o > 0; o >>= 1) tokens += __shfl_xor_sync(0xffffffffu, tokens, o);
   if (e == 0) s_t[r] = tokens;
   __syncthreads();
   if (r == 0) {
     tokens = 0;
-    for (int i = 0; i < BL_THREADS / 32; ++i) { tokens += s_t[i]; if (i) { p += s_p[i * 32 + e]; n += s_n[i * 32 + e]; } }
+    for (int i = 0; i < ROWS; ++i) { tokens += s_t[i]; if (i) { p += s_p[i][e]; n += s_n[i][e]; } }
     const double P = tokens ? p / tokens : 0.0;
     int all = n;
     for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
@@ -191,42 +228,63 @@ static __global__ void __launch_bounds__(BL_THREADS) sh_balance_loss_kernel(cons
 
 // dz, or dz += (ADD: fp32, the gates' gradients of a backward pass).
 template <typename T, int W, int L, bool VEC, bool ADD>
-static __global__ void __launch_bounds__(BL_THREADS) sh_balance_backward_kernel(const BlArgs a) {
+static __global__ void __launch_bounds__(BL_THREADS, 3) sh_balance_backward_kernel(const BlArgs a) {
+  constexpr int AHEAD = BlAhead<T, W>::N;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int row = threadIdx.x / L, at = (threadIdx.x % L) * W;
   const int g0 = blockIdx.y * a.per, gl = row % a.per, tl = row / a.per, gate = g0 + gl;
   const bool mine = tl < a.tpb && gate < a.gates;
   const float gloss = a.gloss ? __ldg(a.gloss) : 1.f;
-  float c[W];
+  float2 c[W / 2];
 #pragma unroll
-  for (int i = 0; i < W; ++i) c[i] = mine && at + i < a.E ? __ldg(a.slope + gate * a.E + at + i) : 0.f;
-  const T* z = (const T*)a.z + (long long)gate * a.E;
-  T* dz = (T*)a.dz + (long long)gate * a.E;
-  for (long long t0 = (long long)blockIdx.x * a.tpb; t0 < a.tokens; t0 += (long long)gridDim.x * a.tpb) {
-    const long long t = t0 + tl;
-    const bool there = mine && t < a.tokens, live = there && (!a.mask || a.mask[t]);
-    float f[W];
+  for (int i = 0; i < W; ++i) (i & 1 ? c[i / 2].y : c[i / 2].x) = mine && at + i < a.E ? __ldg(a.slope + gate * a.E + at + i) : 0.f;
+  const long long step = (long long)gridDim.x * a.tpb;
+  long long t = (long long)blockIdx.x * a.tpb + tl;
+  const T* z = (const T*)a.z + (long long)gate * a.E + at + t * a.zt;
+  T* o = (T*)a.dz + (long long)gate * a.E + at + t * a.dzt;
+  const long long zstep = step * a.zt, ostep = step * a.dzt, rounds = (a.tokens - (long long)blockIdx.x * a.tpb + step - 1) / step;
+  for (long long r = 0; r < rounds; r += AHEAD) {
+    BlRow<T, W, VEC> rows[AHEAD];
+    bool there[AHEAD], live[AHEAD];
 #pragma unroll
-    for (int i = 0; i < W; ++i) f[i] = -INFINITY;
-    if (live) bl_load<T, W, VEC>(z + t * a.zt, at, a.E, f, -INFINITY);
-    bl_softmax<W, L>(f);
-    float dot = 0.f;
+    for (int u = 0; u < AHEAD; ++u) {
+      there[u] = mine && t < a.tokens;
+      live[u] = there[u] && (!a.mask || a.mask[t]);
+      rows[u].load(z, a.E - at, live[u]);
+      t += step; z += zstep;
+    }
 #pragma unroll
-    for (int i = 0; i < W; ++i) dot = fmaf(f[i], c[i], dot);
-    dot = bl_sum<L>(dot);
-    if (!there) continue;                                // (no shuffle below)
+    for (int u = 0; u < AHEAD; ++u) {
+      float2 f[W / 2];
+      rows[u].get(f);
+      const float inv = bl_softmax<W, L>(f);
+      float2 d2 = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < W; ++i) f[i] = live ? gloss * (f[i] * (c[i] - dot)) : 0.f;
-    T* o = dz + t * a.dzt;
-    if constexpr (ADD) {
+      for (int i = 0; i < W / 2; ++i) d2 = __ffma2_rn(f[i], c[i], d2);
+      float dot = d2.x + d2.y;
 #pragma unroll
-      for (int i = 0; i < W; ++i) if (live && at + i < a.E) o[at + i] += f[i];
-    } else if constexpr (VEC) {
-      sh_store<T, W>(o + at, f);
-    } else {
+      for (int q = L / 2; q > 0; q >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, q);
+      dot *= -inv;
+      const float by = gloss * inv;
+      float g[W];
 #pragma unroll
-      for (int i = 0; i < W; ++i) if (at + i < a.E) o[at + i] = sh_from_float<T>(f[i]);
+      for (int i = 0; i < W / 2; ++i) {
+        const float2 v = __fmul2_rn(__fmul2_rn(f[i], make_float2(by, by)), __fadd2_rn(c[i], make_float2(dot, dot)));
+        g[2 * i] = live[u] ? v.x : 0.f; g[2 * i + 1] = live[u] ? v.y : 0.f;
+      }
+      if (there[u]) {
+        if constexpr (ADD) {
+#pragma unroll
+          for (int i = 0; i < W; ++i) if (live[u] && at + i < a.E) o[i] += g[i];
+        } else if constexpr (VEC) {
+          sh_store<T, W>(o, g);
+        } else {
+#pragma unroll
+          for (int i = 0; i < W; ++i) if (at + i < a.E) o[i] = sh_from_float<T>(g[i]);
+        }
+      }
+      o += ostep;
     }
   }
 }

@@ -17,51 +17,84 @@ struct DoArgs {
   float scale;
 };
 
-__device__ __forceinline__ uint4 sh_philox(uint4 c, uint2 k) {
+struct ShPhiloxKey { unsigned k[20]; };     // the keys of the ten rounds
+__device__ __forceinline__ ShPhiloxKey sh_philox_key(unsigned long long seed) {
+  ShPhiloxKey r;
+#pragma unroll
+  for (int i = 0; i < 10; ++i) { r.k[2 * i] = (unsigned)seed + i * 0x9E3779B9u; r.k[2 * i + 1] = (unsigned)(seed >> 32) + i * 0xBB67AE85u; }
+  return r;
+}
+__device__ __forceinline__ uint4 sh_philox(uint4 c, const ShPhiloxKey& key) {
 #pragma unroll
   for (int i = 0; i < 10; ++i) {
     const unsigned long long a = (unsigned long long)c.x * 0xD2511F53u, b = (unsigned long long)c.z * 0xCD9E8D57u;
-    c = make_uint4((unsigned)(b >> 32) ^ c.y ^ k.x, (unsigned)b, (unsigned)(a >> 32) ^ c.w ^ k.y, (unsigned)a);
-    k.x += 0x9E3779B9u; k.y += 0xBB67AE85u;
+    c = make_uint4((unsigned)(b >> 32) ^ c.y ^ key.k[2 * i], (unsigned)b, (unsigned)(a >> 32) ^ c.w ^ key.k[2 * i + 1], (unsigned)a);
   }
   return c;
 }
 
-// A thread takes 8 neighbouring columns, one counter.  VEC: rows of x, residual and y keep 16-byte alignment.
+// A thread takes 8 neighbouring columns, one counter, and two such pieces at a time.  VEC: rows of x, residual and y keep
+// 16-byte alignment.
 template <typename T, bool VEC, bool RES>
 static __global__ void __launch_bounds__(DO_THREADS) sh_dropout_kernel(const DoArgs a) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const unsigned long long seed = __ldg(a.rng), offset = __ldg(a.rng + 1);
-  const unsigned step = gridDim.x * DO_THREADS;
-  for (unsigned u = blockIdx.x * DO_THREADS + threadIdx.x; u < a.units; u += step) {
-    const unsigned r = u / a.upr, blk = u - r * a.upr;
-    const long long row = (long long)a.row0 + r;
-    const int c0 = (int)blk * 8, n = min(8, a.cols - c0);
-    const T* x = (const T*)a.x + row * a.xs + c0;
-    T* y = (T*)a.y + row * a.ys + c0;
-    float f[8], res[8];
-    if (VEC && n == 8) {
-      sh_load<T, 8>(x, f);
-      if constexpr (RES) sh_load<T, 8>((const T*)a.residual + row * a.rs + c0, res);
-    } else {
+  const ShPhiloxKey key = sh_philox_key(seed);
+  const unsigned step = gridDim.x * DO_THREADS, step_r = step / a.upr, step_b = step - step_r * a.upr;
+  unsigned u = blockIdx.x * DO_THREADS + threadIdx.x, r = u / a.upr, blk = u - r * a.upr;
+  const bool all = a.limit > 65535;                      // nothing is kept
+  const unsigned limit = (unsigned)a.limit << 16;
+  constexpr int AHEAD = 2;
+  while (u < a.units) {
+    ShRaw<T, 8> x[AHEAD], res[AHEAD];
+    unsigned rows[AHEAD], blks[AHEAD];
+    bool there[AHEAD];
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) {
+      there[q] = u < a.units;
+      rows[q] = r; blks[q] = blk;
+      if (there[q]) {
+        const long long row = (long long)a.row0 + r;
+        const T* px = (const T*)a.x + row * a.xs + (long long)blk * 8;
+        const T* pr = RES ? (const T*)a.residual + row * a.rs + (long long)blk * 8 : nullptr;
+        const int n = a.cols - (int)blk * 8;
+        if (VEC && n >= 8) {
+          x[q].load(px);
+          if constexpr (RES) res[q].load(pr);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            reinterpret_cast<T*>(x[q].w)[i] = i < n ? px[i] : T(0.f);
+            if constexpr (RES) reinterpret_cast<T*>(res[q].w)[i] = i < n ? pr[i] : T(0.f);
+          }
+        }
+      }
+      u += step; r += step_r; blk += step_b;
+      if (blk >= a.upr) { blk -= a.upr; ++r; }
+    }
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) {
+      if (!there[q]) break;
+      const unsigned row = a.row0 + rows[q];
+      const uint4 w = sh_philox(make_uint4(blks[q], row, (unsigned)offset, (unsigned)(offset >> 32)), key);
+      const unsigned bits[4] = {w.x, w.y, w.z, w.w};
+      float f[8], add[8];
+      x[q].get(f);
+      if constexpr (RES) res[q].get(add);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        f[i] = i < n ? sh_to_float<T>(x[i]) : 0.f;
-        if constexpr (RES) res[i] = i < n ? sh_to_float<T>(((const T*)a.residual)[row * a.rs + c0 + i]) : 0.f;
+        // (the value's 16 bits in the upper half of a word; a dropped value does not count, whatever it is)
+        const unsigned v = i & 1 ? bits[i / 2] : bits[i / 2] << 16;
+        const float d = !all && v >= limit ? f[i] * a.scale : 0.f;
+        f[i] = RES ? d + add[i] : d;
       }
-    }
-    const uint4 w = sh_philox(make_uint4(blk, (unsigned)row, (unsigned)offset, (unsigned)(offset >> 32)), make_uint2((unsigned)seed, (unsigned)(seed >> 32)));
-    const unsigned bits[4] = {w.x, w.y, w.z, w.w};
+      T* y = (T*)a.y + (long long)row * a.ys + (long long)blks[q] * 8;
+      const int n = a.cols - (int)blks[q] * 8;
+      if (VEC && n >= 8) sh_store<T, 8>(y, f);
+      else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int v = (int)(i & 1 ? bits[i / 2] >> 16 : bits[i / 2] & 0xFFFFu);
-      const float d = v >= a.limit ? f[i] * a.scale : 0.f;       // (a dropped value does not count, whatever it is)
-      f[i] = RES ? d + res[i] : d;
-    }
-    if (VEC && n == 8) sh_store<T, 8>(y, f);
-    else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) if (i < n) y[i] = sh_from_float<T>(f[i]);
+        for (int i = 0; i < 8; ++i) if (i < n) y[i] = sh_from_float<T>(f[i]);
+      }
     }
   }
 }

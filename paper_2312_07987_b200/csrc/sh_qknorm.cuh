@@ -8,11 +8,12 @@
 // same lane.  A group takes several heads of one token, which share the angles.
 //
 // Angles are turns in 64-bit fixed point: the frequency (divided by 2 pi) times the position, modulo 2^64, is the fraction
-// of a turn without any rounding that grows with the position; sincospif of its upper 32 bits is off by 2^-25 turns at most.
+// of a turn without any rounding that grows with the position; its upper 32 bits as a float are off by 2^-26 turns at most.
 #pragma once
 #include "sh_vec.cuh"
 
 constexpr int QN_THREADS = 256;
+
 constexpr int QN_MAX_D = 256;
 constexpr int QN_MAX_BLOCKS = 1024;       // blocks of the backward kernel at most (rows of its partial gain gradients)
 
@@ -65,38 +66,54 @@ __device__ __forceinline__ void qn_columns(const QnArgs& a, int l, int (&col)[NV
   }
 }
 
-// cos and sin of a lane's pairs at a position: pair p of a vector (neighbouring) or of two vectors (halves).
-template <int V, int NV, bool PAIRED>
-__device__ __forceinline__ void qn_angles(const QnArgs& a, const unsigned long long* freq, long long pos, const int (&col)[NV], float (&cs)[NV * V / 2], float (&sn)[NV * V / 2]) {
+// The lane's values as pairs (A, B) that a rotation mixes, two pairs to a register pair (packed fp32 arithmetic: two
+// operations an instruction).  Pair n is made of two neighbouring values, or of value n % V of vectors 2 (n / V) and + 1.
+template <int V, bool PAIRED> __device__ __forceinline__ constexpr int qn_vec_a(int n) { return PAIRED ? 2 * (n / V) : 2 * n / V; }
+template <int V, bool PAIRED> __device__ __forceinline__ constexpr int qn_vec_b(int n) { return PAIRED ? 2 * (n / V) + 1 : (2 * n + 1) / V; }
+template <int V, bool PAIRED> __device__ __forceinline__ constexpr int qn_at_a(int n) { return PAIRED ? n % V : 2 * n % V; }
+template <int V, bool PAIRED> __device__ __forceinline__ constexpr int qn_at_b(int n) { return PAIRED ? n % V : (2 * n + 1) % V; }
+
+template <int P> struct QnPairs { float2 a[P / 2], b[P / 2]; };
+
+__device__ __forceinline__ float& qn_half(float2& v, int h) { return h ? v.y : v.x; }
+
+template <typename T, int V, int NV, bool PAIRED>
+__device__ __forceinline__ void qn_get(const ShRaw<T, V> (&raw)[NV], QnPairs<NV * V / 2>& x) {
+  float f[NV][V];
 #pragma unroll
-  for (int i = 0; i < NV * V / 2; ++i) {
-    int pair, at;                                        // the pair's number and its first column
-    bool rot;
-    if constexpr (PAIRED) {
-      const bool next = V == 1 && a.next;
-      at = col[2 * (i / V)] + i % V; pair = next ? at / 2 : at;
-      rot = col[2 * (i / V)] >= 0 && pair < a.R / 2;
-    } else {
-      at = col[i / (V / 2)] + 2 * (i % (V / 2)); pair = at / 2;
-      rot = col[i / (V / 2)] >= 0 && at < a.R;
-    }
-    cs[i] = 1.f; sn[i] = 0.f;
-    if (rot) {
-      const unsigned long long turns = (unsigned long long)pos * freq[pair];
-      sincospif((float)(int)(turns >> 32) * 4.656612873077393e-10f, &sn[i], &cs[i]);   // (2^-31: half turns)
-    }
+  for (int i = 0; i < NV; ++i) raw[i].get(f[i]);
+#pragma unroll
+  for (int n = 0; n < NV * V / 2; ++n) {
+    qn_half(x.a[n / 2], n & 1) = f[qn_vec_a<V, PAIRED>(n)][qn_at_a<V, PAIRED>(n)];
+    qn_half(x.b[n / 2], n & 1) = f[qn_vec_b<V, PAIRED>(n)][qn_at_b<V, PAIRED>(n)];
   }
 }
-
-template <int V, int NV, bool PAIRED, bool BACK>
-__device__ __forceinline__ void qn_rotate(float (&f)[NV][V], const float (&cs)[NV * V / 2], const float (&sn)[NV * V / 2]) {
+template <typename T, int V, int NV, bool PAIRED>
+__device__ __forceinline__ void qn_put(T* const (&p)[NV], const int (&col)[NV], QnPairs<NV * V / 2>& x) {
+  float f[NV][V];
 #pragma unroll
-  for (int i = 0; i < NV * V / 2; ++i) {
-    float& p = PAIRED ? f[2 * (i / V)][i % V] : f[i / (V / 2)][2 * (i % (V / 2))];
-    float& q = PAIRED ? f[2 * (i / V) + 1][i % V] : f[i / (V / 2)][2 * (i % (V / 2)) + 1];
-    const float s = BACK ? -sn[i] : sn[i], x = p, y = q;
-    p = x * cs[i] - y * s;
-    q = x * s + y * cs[i];
+  for (int n = 0; n < NV * V / 2; ++n) {
+    f[qn_vec_a<V, PAIRED>(n)][qn_at_a<V, PAIRED>(n)] = qn_half(x.a[n / 2], n & 1);
+    f[qn_vec_b<V, PAIRED>(n)][qn_at_b<V, PAIRED>(n)] = qn_half(x.b[n / 2], n & 1);
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (col[i] >= 0) sh_store<T, V>(p[i], f[i]);
+}
+
+// cos and sin of pair n at a position: 1 and 0 behind the rotated columns.  16-bit results: the special function unit's (off by
+// 2^-21, where a result's half step is 2^-12 at least); fp32: sincospif.
+template <typename T, int V, int NV, bool PAIRED>
+__device__ __forceinline__ void qn_angle(const QnArgs& a, const unsigned long long* freq, long long pos, const int (&col)[NV], int n, float* cs, float* sn) {
+  const int c = col[qn_vec_a<V, PAIRED>(n)], at = c + qn_at_a<V, PAIRED>(n);
+  const bool next = !PAIRED || (V == 1 && a.next);
+  const int pair = next ? at / 2 : at;
+  *cs = 1.f; *sn = 0.f;
+  if (c >= 0 && pair < a.R / 2) {
+    const unsigned long long turns = (unsigned long long)pos * freq[pair];
+    const float x = (float)(int)(turns >> 32);           // half turns times 2^31
+    if constexpr (sizeof(T) == 2) __sincosf(x * (3.14159265f * 4.656612873077393e-10f), sn, cs);
+    else sincospif(x * 4.656612873077393e-10f, sn, cs);
   }
 }
 
@@ -104,15 +121,14 @@ __device__ __forceinline__ long long qn_position(const QnArgs& a, long long toke
   if (!a.pos) return t;
   return a.pos64 ? __ldg((const long long*)a.pos + token) : (long long)__ldg((const int*)a.pos + token);
 }
-
 __device__ __forceinline__ long long qn_div(long long n, int d) { return n >> 32 ? n / d : (long long)((unsigned)n / (unsigned)d); }
 
 // V = 1 without pairs: nothing is rotated (d_head may be odd).
 template <typename T, int V, int NV, bool PAIRED>
-static __global__ void __launch_bounds__(QN_THREADS) sh_qk_norm_kernel(const __grid_constant__ QnArgs a) {
+static __global__ void __launch_bounds__(QN_THREADS, 3) sh_qk_norm_kernel(const __grid_constant__ QnArgs a) {
   __shared__ unsigned long long s_freq[QN_MAX_D / 2];
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  constexpr int P = V > 1 || PAIRED ? NV * V / 2 : 1;
+  constexpr int P = NV * V / 2;
   for (int i = threadIdx.x; i < a.R / 2; i += QN_THREADS) s_freq[i] = a.freq[i];
   if (a.R) __syncthreads();
   const int l = threadIdx.x & (a.lanes - 1);
@@ -126,53 +142,64 @@ static __global__ void __launch_bounds__(QN_THREADS) sh_qk_norm_kernel(const __g
   if (side) chunk -= a.s[0].chunks;
   const long long b = qn_div(token, a.seq);
   const int t = (int)(token - b * a.seq);
+  const int h0 = chunk * a.per, n = live ? min(a.per, s.heads - h0) : 0;
   int col[NV];
   qn_columns<V, NV, PAIRED>(a, l, col);
-  float cs[P], sn[P];
-  if constexpr (V > 1 || PAIRED)
-    if (a.R && live) qn_angles<V, NV, PAIRED>(a, s_freq, qn_position(a, token, t), col, cs, sn);
-  float g[NV][V];
+  const T* px[NV];
+  T* py[NV];
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
+  for (int i = 0; i < NV; ++i) {
+    px[i] = (const T*)s.x + b * s.xb + t * s.xt + h0 * s.xh + col[i];
+    py[i] = (T*)s.out + b * s.ob + t * s.ot + h0 * s.oh + col[i];
+  }
+  // the next two heads' values are on their way while one is worked on; the same number of rounds for every group of a warp
+  ShRaw<T, V> raw[2][NV];
+  auto fetch = [&](int j) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) g[i][j] = s.scale * (s.gain && col[i] >= 0 ? __ldg(s.gain + col[i] + j) : 1.f);
-  const T* x = (const T*)s.x + b * s.xb + t * s.xt;
-  T* y = (T*)s.out + b * s.ob + t * s.ot;
-  const int h0 = chunk * a.per;
+    for (int i = 0; i < NV; ++i) {
+      if (j < n && col[i] >= 0) raw[j & 1][i].load(px[i]);
+      else raw[j & 1][i].fill(0);
+      px[i] += s.xh;
+    }
+  };
+  fetch(0); fetch(1);
+  // y = r (A ga cs - B gb sn, A ga sn + B gb cs): gains, scale and angles in four factors a pair, for all of the heads
+  QnPairs<P> fa, fb;
+#pragma unroll
+  for (int m = 0; m < P; ++m) {
+    float cs = 1.f, sn = 0.f;
+    if constexpr (V > 1 || PAIRED)
+      if (a.R && live) qn_angle<T, V, NV, PAIRED>(a, s_freq, qn_position(a, token, t), col, m, &cs, &sn);
+    const int ca = col[qn_vec_a<V, PAIRED>(m)], cb = col[qn_vec_b<V, PAIRED>(m)];
+    const float ga = s.scale * (s.gain && ca >= 0 ? __ldg(s.gain + ca + qn_at_a<V, PAIRED>(m)) : 1.f);
+    const float gb = s.scale * (s.gain && cb >= 0 ? __ldg(s.gain + cb + qn_at_b<V, PAIRED>(m)) : 1.f);
+    qn_half(fa.a[m / 2], m & 1) = ga * cs; qn_half(fa.b[m / 2], m & 1) = -gb * sn;
+    qn_half(fb.a[m / 2], m & 1) = ga * sn; qn_half(fb.b[m / 2], m & 1) = gb * cs;
+  }
   const float inv = 1.f / (float)a.D;
-  // the same number of rounds for every group of a warp; two heads' loads in flight
-  for (int j = 0; j < a.per; j += 2) {
-    float f[2][NV][V];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        if (live && h0 + j + u < s.heads && j + u < a.per && col[i] >= 0) {
-          sh_load<T, V>(x + (h0 + j + u) * s.xh + col[i], f[u][i]);
-        } else {
-#pragma unroll
-          for (int v = 0; v < V; ++v) f[u][i][v] = 0.f;
-        }
-      }
+  for (int j0 = 0; j0 < a.per; j0 += 2) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      float ss = 0.f;
+      const int j = j0 + u;
+      if (j >= a.per) break;
+      QnPairs<P> x, y;
+      qn_get<T, V, NV, PAIRED>(raw[u], x);
+      fetch(j0 + 2 + u);
+      float2 ss = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int v = 0; v < V; ++v) ss = fmaf(f[u][i][v], f[u][i][v], ss);
-      const float r = rsqrtf(fmaf(sh_group_sum(ss, a.lanes), inv, a.eps));
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int v = 0; v < V; ++v) f[u][i][v] *= r * g[i][v];
-      if constexpr (V > 1 || PAIRED)
-        if (a.R) qn_rotate<V, NV, PAIRED, false>(f[u], cs, sn);
-      if (live && h0 + j + u < s.heads && j + u < a.per) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-          if (col[i] >= 0) sh_store<T, V>(y + (h0 + j + u) * s.oh + col[i], f[u][i]);
+      for (int m = 0; m < P / 2; ++m) {
+        ss = __ffma2_rn(x.a[m], x.a[m], ss);
+        ss = __ffma2_rn(x.b[m], x.b[m], ss);
+        y.a[m] = __ffma2_rn(x.a[m], fa.a[m], __fmul2_rn(x.b[m], fa.b[m]));
+        y.b[m] = __ffma2_rn(x.a[m], fb.a[m], __fmul2_rn(x.b[m], fb.b[m]));
       }
+      const float r = rsqrtf(fmaf(sh_group_sum(ss.x + ss.y, a.lanes), inv, a.eps));
+      const float2 rr = make_float2(r, r);
+#pragma unroll
+      for (int m = 0; m < P / 2; ++m) { y.a[m] = __fmul2_rn(y.a[m], rr); y.b[m] = __fmul2_rn(y.b[m], rr); }
+      if (j < n) qn_put<T, V, NV, PAIRED>(py, col, y);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) py[i] += s.oh;
     }
   }
 }
@@ -181,12 +208,12 @@ static __global__ void __launch_bounds__(QN_THREADS) sh_qk_norm_kernel(const __g
 // A thread adds its columns' share of the gain gradients over its rows; the block's groups are added in order in shared
 // memory, the blocks by sh_qk_norm_gain_kernel: the same bits on every run.
 template <typename T, int V, int NV, bool PAIRED>
-static __global__ void __launch_bounds__(QN_THREADS) sh_qk_norm_backward_kernel(const __grid_constant__ QnArgs a) {
+static __global__ void __launch_bounds__(QN_THREADS, 2) sh_qk_norm_backward_kernel(const __grid_constant__ QnArgs a) {
   __shared__ unsigned long long s_freq[QN_MAX_D / 2];
   extern __shared__ float s_sum[];                       // [groups][D]
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  constexpr int P = V > 1 || PAIRED ? NV * V / 2 : 1;
+  constexpr int P = NV * V / 2;
   for (int i = threadIdx.x; i < a.R / 2; i += QN_THREADS) s_freq[i] = a.freq[i];
   if (a.R) __syncthreads();
   const int l = threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes, groups = QN_THREADS / a.lanes;
@@ -195,14 +222,14 @@ static __global__ void __launch_bounds__(QN_THREADS) sh_qk_norm_backward_kernel(
   const int block = side ? blockIdx.x - a.blocks0 : blockIdx.x, blocks = side ? gridDim.x - a.blocks0 : a.blocks0;
   int col[NV];
   qn_columns<V, NV, PAIRED>(a, l, col);
-  float g[NV][V], dg[NV][V];
+  QnPairs<P> g, dg;
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      g[i][j] = s.gain && col[i] >= 0 ? __ldg(s.gain + col[i] + j) : 1.f;
-      dg[i][j] = 0.f;
-    }
+  for (int m = 0; m < P; ++m) {
+    const int ca = col[qn_vec_a<V, PAIRED>(m)], cb = col[qn_vec_b<V, PAIRED>(m)];
+    qn_half(g.a[m / 2], m & 1) = s.gain && ca >= 0 ? __ldg(s.gain + ca + qn_at_a<V, PAIRED>(m)) : 1.f;
+    qn_half(g.b[m / 2], m & 1) = s.gain && cb >= 0 ? __ldg(s.gain + cb + qn_at_b<V, PAIRED>(m)) : 1.f;
+    qn_half(dg.a[m / 2], m & 1) = qn_half(dg.b[m / 2], m & 1) = 0.f;
+  }
   const float inv = 1.f / (float)a.D;
   const long long items = a.tokens * s.chunks, step = (long long)blocks * groups;
   // (rounds: the same for every group of the block)
@@ -210,64 +237,78 @@ static __global__ void __launch_bounds__(QN_THREADS) sh_qk_norm_backward_kernel(
     const long long item = first + group;
     const bool live = item < items;
     const long long token = live ? qn_div(item, s.chunks) : 0;
-    const int h0 = live ? (int)(item - token * s.chunks) * a.per : 0;
+    const int h0 = live ? (int)(item - token * s.chunks) * a.per : 0, n = live ? min(a.per, s.heads - h0) : 0;
     const long long b = qn_div(token, a.seq);
     const int t = (int)(token - b * a.seq);
-    float cs[P], sn[P];
-    if constexpr (V > 1 || PAIRED)
-      if (a.R && live) qn_angles<V, NV, PAIRED>(a, s_freq, qn_position(a, token, t), col, cs, sn);
-    const T* x = (const T*)s.x + b * s.xb + t * s.xt;
-    const T* dy = (const T*)s.dy + b * s.yb + t * s.yt;
-    T* dx = (T*)s.out + b * s.ob + t * s.ot;
-    for (int j = 0; j < a.per; ++j) {
-      const int h = h0 + j;
-      const bool row = live && h < s.heads;
-      float f[NV][V], u[NV][V];
+    const T *px[NV], *py[NV];
+    T* po[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      px[i] = (const T*)s.x + b * s.xb + t * s.xt + h0 * s.xh + col[i];
+      py[i] = (const T*)s.dy + b * s.yb + t * s.yt + h0 * s.yh + col[i];
+      po[i] = (T*)s.out + b * s.ob + t * s.ot + h0 * s.oh + col[i];
+    }
+    // the next head's values are on their way while one is worked on
+    ShRaw<T, V> rx[NV], ry[NV];
+    auto fetch = [&](int j) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        if (row && col[i] >= 0) {
-          sh_load<T, V>(x + h * s.xh + col[i], f[i]);
-          sh_load<T, V>(dy + h * s.yh + col[i], u[i]);
-        } else {
-#pragma unroll
-          for (int v = 0; v < V; ++v) f[i][v] = u[i][v] = 0.f;
-        }
+        if (j < n && col[i] >= 0) { rx[i].load(px[i]); ry[i].load(py[i]); }
+        else { rx[i].fill(0); ry[i].fill(0); }
+        px[i] += s.xh; py[i] += s.yh;
       }
+    };
+    fetch(0);
+    float2 cs[P / 2], sn[P / 2];                         // times the scale
+#pragma unroll
+    for (int m = 0; m < P; ++m) {
+      float c = 1.f, d = 0.f;
       if constexpr (V > 1 || PAIRED)
-        if (a.R) qn_rotate<V, NV, PAIRED, true>(u, cs, sn);
-      float ss = 0.f, wx = 0.f;
+        if (a.R && live) qn_angle<T, V, NV, PAIRED>(a, s_freq, qn_position(a, token, t), col, m, &c, &d);
+      qn_half(cs[m / 2], m & 1) = s.scale * c; qn_half(sn[m / 2], m & 1) = s.scale * d;
+    }
+    for (int j = 0; j < a.per; ++j) {
+      QnPairs<P> x, y, u;
+      qn_get<T, V, NV, PAIRED>(rx, x);
+      qn_get<T, V, NV, PAIRED>(ry, y);
+      fetch(j + 1);
+      // u = s Rot(-pos) dy;  t = u x;  sums of x^2 and of g t;  dx = r (g u) - r m x
+      float2 ss = make_float2(0.f, 0.f), wx = ss;
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          u[i][v] *= s.scale;
-          ss = fmaf(f[i][v], f[i][v], ss);
-          wx = fmaf(u[i][v] * g[i][v], f[i][v], wx);
-        }
-      ss = sh_group_sum(ss, a.lanes);
-      wx = sh_group_sum(wx, a.lanes);
-      const float r = rsqrtf(fmaf(ss, inv, a.eps)), m = wx * inv * r * r;
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          if (row) dg[i][v] = fmaf(u[i][v], f[i][v] * r, dg[i][v]);
-          u[i][v] = r * fmaf(-f[i][v], m, u[i][v] * g[i][v]);
-        }
-      if (row) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-          if (col[i] >= 0) sh_store<T, V>(dx + h * s.oh + col[i], u[i]);
+      for (int m = 0; m < P / 2; ++m) {
+        u.a[m] = __ffma2_rn(y.a[m], cs[m], __fmul2_rn(y.b[m], sn[m]));
+        u.b[m] = __ffma2_rn(y.b[m], cs[m], __fmul2_rn(y.a[m], make_float2(-sn[m].x, -sn[m].y)));
+        ss = __ffma2_rn(x.a[m], x.a[m], ss);
+        ss = __ffma2_rn(x.b[m], x.b[m], ss);
+        y.a[m] = __fmul2_rn(u.a[m], x.a[m]);
+        y.b[m] = __fmul2_rn(u.b[m], x.b[m]);
+        wx = __ffma2_rn(y.a[m], g.a[m], wx);
+        wx = __ffma2_rn(y.b[m], g.b[m], wx);
+        u.a[m] = __fmul2_rn(u.a[m], g.a[m]);
+        u.b[m] = __fmul2_rn(u.b[m], g.b[m]);
       }
+      const float sum = sh_group_sum(ss.x + ss.y, a.lanes), dot = sh_group_sum(wx.x + wx.y, a.lanes);
+      const float r = rsqrtf(fmaf(sum, inv, a.eps)), rm = -(dot * inv * r * r) * r;
+      const float2 r2 = make_float2(r, r), rm2 = make_float2(rm, rm);
+#pragma unroll
+      for (int m = 0; m < P / 2; ++m) {
+        dg.a[m] = __ffma2_rn(y.a[m], r2, dg.a[m]);       // (no row: zeros)
+        dg.b[m] = __ffma2_rn(y.b[m], r2, dg.b[m]);
+        u.a[m] = __ffma2_rn(x.a[m], rm2, __fmul2_rn(u.a[m], r2));
+        u.b[m] = __ffma2_rn(x.b[m], rm2, __fmul2_rn(u.b[m], r2));
+      }
+      if (j < n) qn_put<T, V, NV, PAIRED>(po, col, u);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) po[i] += s.oh;
     }
   }
   if (!s.dgain) return;                                  // (the whole block)
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
-    if (col[i] >= 0) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) s_sum[group * a.D + col[i] + v] = dg[i][v];
-    }
+  for (int m = 0; m < P; ++m) {
+    const int ca = col[qn_vec_a<V, PAIRED>(m)], cb = col[qn_vec_b<V, PAIRED>(m)];
+    if (ca >= 0) s_sum[group * a.D + ca + qn_at_a<V, PAIRED>(m)] = qn_half(dg.a[m / 2], m & 1);
+    if (cb >= 0) s_sum[group * a.D + cb + qn_at_b<V, PAIRED>(m)] = qn_half(dg.b[m / 2], m & 1);
+  }
   __syncthreads();
   for (int c = threadIdx.x; c < a.D; c += QN_THREADS) {
     float sum = 0.f;
@@ -286,6 +327,7 @@ static __global__ void __launch_bounds__(1024) sh_qk_norm_gain_kernel(QnGain a) 
   if (!out) return;                                      // (the whole block)
   double sum = 0.0;
   if (c < a.D)
+#pragma unroll 8
     for (int i = a.first[side] + threadIdx.y; i < a.first[side + 1]; i += 32) sum += (double)__ldcg(a.part + (long long)i * a.D + c);
   s_sum[threadIdx.y][threadIdx.x] = sum;
   __syncthreads();

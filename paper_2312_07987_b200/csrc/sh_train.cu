@@ -38,12 +38,6 @@ int pow2_at_least(int n) { int p = 1; while (p < n) p *= 2; return p; }
 
 // ---- norms of queries and keys ----
 
-bool heads_ok(const char* what, const sh_heads& h) {
-  if (h.heads < 0) { sh_set_error("%s: heads must not be negative (got %d)", what, h.heads); return false; }
-  if (h.heads > 0 && !h.data) { sh_set_error("%s: data must not be NULL", what); return false; }
-  return true;
-}
-
 // Two elements of an output at one address: a dimension of more than one has no stride.
 bool apart(const char* what, std::initializer_list<std::pair<long long, long long>> dims) {
   for (auto& d : dims)
@@ -52,66 +46,59 @@ bool apart(const char* what, std::initializer_list<std::pair<long long, long lon
 }
 
 // Values a vector may have: every address and every run of columns is a multiple of it.
-int vector_width(const sh_qk_norm_args& a, bool backward) {
+int vector_width(const sh_qk_norm_args& a, const sh_qk_norm_backward_args* back) {
   const int size = (int)elem_bytes(a.dtype);
+  long long all = a.d_head;                                // (what has to be a multiple: a power of two of it is its lowest bit)
+  if (a.rotated && a.halves) all |= a.rotated / 2 | (a.d_head - a.rotated) / 2;
+  auto add = [&](const sh_heads& h, int heads) {
+    if (heads == 0) return;
+    all |= (long long)((uintptr_t)h.data / size);
+    if (a.batch > 1) all |= h.batch_stride;
+    if (a.seq > 1) all |= h.token_stride;
+    if (heads > 1) all |= h.head_stride;
+  };
+  add(a.q, a.q_heads); add(a.q_out, a.q_heads); add(a.k, a.k_heads); add(a.k_out, a.k_heads);
+  if (back) { add(back->dq, a.q_heads); add(back->dk, a.k_heads); }
   int v = 16 / size;
-  auto fits = [&](long long n) { while (v > 1 && n % v) v /= 2; };
-  fits(a.d_head);
-  if (a.rotated && a.halves) { fits(a.rotated / 2); fits((a.d_head - a.rotated) / 2); }
-  const sh_heads* t[] = {&a.q, &a.k, &a.q_out, &a.k_out, &a.dq, &a.dk};
-  for (int i = 0; i < (backward ? 6 : 4); ++i) {
-    const sh_heads& h = *t[i];
-    const int heads = i % 2 ? a.k.heads : a.q.heads;
-    if (heads == 0) continue;
-    fits((long long)((uintptr_t)h.data / size));
-    if (a.batch > 1) fits(h.batch_stride);
-    if (a.seq > 1) fits(h.token_stride);
-    if (heads > 1) fits(h.head_stride);
-  }
+  while (all & (v - 1)) v /= 2;
   return v;
 }
 
-int qn_check(const sh_qk_norm_args* p, bool backward) {
-  sh_set_error("%s", "");
-  if (!p) { sh_set_error("args is NULL"); return SH_ERR_INVALID_ARG; }
-  const sh_qk_norm_args& a = *p;
+int qn_check(const sh_qk_norm_args& a, const sh_qk_norm_backward_args* back) {
   if (!dtype_ok(a.dtype, true)) return SH_ERR_INVALID_ARG;
   if (a.batch < 0 || a.seq < 0) { sh_set_error("batch and seq must not be negative (got %d, %d)", a.batch, a.seq); return SH_ERR_INVALID_ARG; }
+  if (a.q_heads < 0 || a.k_heads < 0) { sh_set_error("q_heads and k_heads must not be negative (got %d, %d)", a.q_heads, a.k_heads); return SH_ERR_INVALID_ARG; }
   if (a.d_head < 1 || a.d_head > QN_MAX_D) { sh_set_error("d_head must be in 1..%d (got %d)", QN_MAX_D, a.d_head); return SH_ERR_INVALID_ARG; }
   if (a.rotated < 0 || a.rotated > a.d_head || a.rotated % 2) { sh_set_error("rotated must be even and in 0..d_head (got %d, d_head %d)", a.rotated, a.d_head); return SH_ERR_INVALID_ARG; }
   if (a.rotated && a.d_head % 2) { sh_set_error("a rotation needs an even d_head (got %d)", a.d_head); return SH_ERR_UNSUPPORTED; }
   if (a.rotated && !(a.base > 0.0 && std::isfinite(a.base))) { sh_set_error("rotary base must be positive and finite (got %g)", a.base); return SH_ERR_INVALID_ARG; }
   if (!(a.eps > 0.f && std::isfinite(a.eps))) { sh_set_error("eps must be positive and finite (got %g)", (double)a.eps); return SH_ERR_INVALID_ARG; }
   if (!std::isfinite(a.q_scale)) { sh_set_error("q_scale must be finite (got %g)", (double)a.q_scale); return SH_ERR_INVALID_ARG; }
-  if (a.batch == 0 || a.seq == 0) {
-    if (a.q.heads < 0 || a.k.heads < 0) { sh_set_error("heads must not be negative (got %d, %d)", a.q.heads, a.k.heads); return SH_ERR_INVALID_ARG; }
-    return SH_OK;
+  if (a.batch == 0 || a.seq == 0) return SH_OK;
+  struct Side { const char *in, *out; const sh_heads &x, &y; const sh_heads* dy; int heads; };
+  const Side sides[2] = {{"q", "q_out", a.q, a.q_out, back ? &back->dq : nullptr, a.q_heads}, {"k", "k_out", a.k, a.k_out, back ? &back->dk : nullptr, a.k_heads}};
+  for (const Side& s : sides) {
+    if (s.heads == 0) continue;
+    if (!s.x.data || !s.y.data) { sh_set_error("%s and %s must not be NULL", s.in, s.out); return SH_ERR_INVALID_ARG; }
+    if (s.dy && !s.dy->data) { sh_set_error("d%s must not be NULL", s.in); return SH_ERR_INVALID_ARG; }
+    for (const sh_heads* h : {&s.x, &s.y, s.dy})
+      if (h && (uintptr_t)h->data % elem_bytes(a.dtype)) { sh_set_error("%s, %s or d%s is not aligned to its elements", s.in, s.out, s.in); return SH_ERR_INVALID_ARG; }
+    if (!apart(s.out, {{a.batch, s.y.batch_stride}, {a.seq, s.y.token_stride}, {s.heads, s.y.head_stride}})) return SH_ERR_INVALID_ARG;
   }
-  if (!heads_ok("q", a.q) || !heads_ok("k", a.k)) return SH_ERR_INVALID_ARG;
-  const sh_heads *oq = &a.q_out, *ok = &a.k_out;
-  if ((a.q.heads && !oq->data) || (a.k.heads && !ok->data)) { sh_set_error("q_out and k_out must not be NULL"); return SH_ERR_INVALID_ARG; }
-  if (a.q.heads && !apart("q_out", {{a.batch, oq->batch_stride}, {a.seq, oq->token_stride}, {a.q.heads, oq->head_stride}})) return SH_ERR_INVALID_ARG;
-  if (a.k.heads && !apart("k_out", {{a.batch, ok->batch_stride}, {a.seq, ok->token_stride}, {a.k.heads, ok->head_stride}})) return SH_ERR_INVALID_ARG;
-  if (backward && ((a.q.heads && !a.dq.data) || (a.k.heads && !a.dk.data))) { sh_set_error("dq and dk must not be NULL"); return SH_ERR_INVALID_ARG; }
   return SH_OK;
 }
 
-// The kernel's arguments; `per` heads to a group.
-void qn_fill(const sh_qk_norm_args& p, bool backward, int v, int nv, QnArgs& a) {
-  const sh_heads* in[2] = {&p.q, &p.k};
-  const sh_heads* out[2] = {&p.q_out, &p.k_out};
-  const sh_heads* dy[2] = {&p.dq, &p.dk};
-  for (int i = 0; i < 2; ++i) {
-    QnSide& s = a.s[i];
-    s.x = in[i]->data; s.xb = in[i]->batch_stride; s.xt = in[i]->token_stride; s.xh = in[i]->head_stride;
-    s.out = out[i]->data; s.ob = out[i]->batch_stride; s.ot = out[i]->token_stride; s.oh = out[i]->head_stride;
-    s.dy = nullptr; s.yb = s.yt = s.yh = 0;
-    if (backward) { s.dy = dy[i]->data; s.yb = dy[i]->batch_stride; s.yt = dy[i]->token_stride; s.yh = dy[i]->head_stride; }
-    s.gain = i ? p.gk : p.gq;
-    s.dgain = backward ? (i ? p.dgk : p.dgq) : nullptr;
-    s.heads = in[i]->heads;
-    s.scale = i ? 1.f : p.q_scale;
-  }
+// The kernel's arguments, for vectors of v values.
+void qn_fill(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, int v, int nv, QnArgs& a) {
+  const sh_heads none{};
+  auto side = [&](QnSide& s, const sh_heads& x, const sh_heads& out, const sh_heads& dy, const float* gain, float* dgain, int heads, float scale) {
+    s.x = x.data; s.xb = x.batch_stride; s.xt = x.token_stride; s.xh = x.head_stride;
+    s.out = out.data; s.ob = out.batch_stride; s.ot = out.token_stride; s.oh = out.head_stride;
+    s.dy = dy.data; s.yb = dy.batch_stride; s.yt = dy.token_stride; s.yh = dy.head_stride;
+    s.gain = gain; s.dgain = dgain; s.heads = heads; s.scale = scale;
+  };
+  side(a.s[0], p.q, p.q_out, back ? back->dq : none, p.gq, back ? back->dgq : nullptr, p.q_heads, p.q_scale);
+  side(a.s[1], p.k, p.k_out, back ? back->dk : none, p.gk, back ? back->dgk : nullptr, p.k_heads, 1.f);
   a.pos = p.positions; a.pos64 = p.positions_64 != 0;
   a.next = p.rotated && !p.halves;
   a.seq = p.seq; a.D = p.d_head; a.R = p.rotated;
@@ -145,14 +132,15 @@ int qn_dispatch(const QnArgs& a, int v, bool halves, bool backward, bool pdl, in
   return a.R ? qn_launch<T, 1, 8, true>(a, backward, pdl, blocks, smem, st) : qn_launch<T, 1, 8, false>(a, backward, pdl, blocks, smem, st);
 }
 
-int qn_run(const sh_qk_norm_args& p, bool backward, bool pdl, cudaStream_t st) {
+int qn_run(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, bool pdl, cudaStream_t st) {
+  const bool backward = back != nullptr;
   int sms = 0;
   if (int rc = device_sms(&sms)) return rc;
   const bool halves = p.rotated && p.halves;
-  const int v = vector_width(p, backward);
+  const int v = vector_width(p, back);
   QnArgs a;
-  qn_fill(p, backward, v, qn_vectors(v), a);
-  const int groups = QN_THREADS / a.lanes, most = p.q.heads > p.k.heads ? p.q.heads : p.k.heads;
+  qn_fill(p, back, v, qn_vectors(v), a);
+  const int groups = QN_THREADS / a.lanes, most = p.q_heads > p.k_heads ? p.q_heads : p.k_heads;
   // heads to a group: all of them share a token's angles, but not so many that SMs are left without work
   a.per = most < 8 ? (most < 1 ? 1 : most) : 8;
   auto chunks = [&](int i) { return (a.s[i].heads + a.per - 1) / a.per; };
@@ -164,7 +152,7 @@ int qn_run(const sh_qk_norm_args& p, bool backward, bool pdl, cudaStream_t st) {
   if (backward) {
     long long n[2];
     for (int i = 0; i < 2; ++i) n[i] = (items[i] + groups - 1) / groups;
-    const long long cap = 4ll * sms < QN_MAX_BLOCKS ? 4ll * sms : QN_MAX_BLOCKS;
+    const long long cap = 2ll * sms < QN_MAX_BLOCKS ? 2ll * sms : QN_MAX_BLOCKS;
     if (n[0] + n[1] > cap) {                               // shares by the sides' rows
       const long long all = n[0] + n[1];
       const long long b0 = n[0] ? (n[0] * cap + all / 2) / all : 0;
@@ -173,7 +161,7 @@ int qn_run(const sh_qk_norm_args& p, bool backward, bool pdl, cudaStream_t st) {
     }
     a.blocks0 = (int)n[0];
     blocks = n[0] + n[1];
-    a.part = (float*)p.workspace;
+    a.part = (float*)back->workspace;
     smem = (size_t)groups * p.d_head * 4;
   }
   if (blocks > 0x7fffffffll) { sh_set_error("too many rows: batch * seq * heads / %d must be below 2^31", groups); return SH_ERR_UNSUPPORTED; }
@@ -183,8 +171,8 @@ int qn_run(const sh_qk_norm_args& p, bool backward, bool pdl, cudaStream_t st) {
                                 : qn_dispatch<__half>(a, v, halves, backward, pdl, (int)blocks, smem, st);
     if (rc) return rc;
   }
-  if (backward && (p.dgq || p.dgk)) {
-    QnGain g{a.part, {p.dgq, p.dgk}, {0, a.blocks0, (int)blocks}, p.d_head};
+  if (backward && (back->dgq || back->dgk)) {
+    QnGain g{a.part, {back->dgq, back->dgk}, {0, a.blocks0, (int)blocks}, p.d_head};
     return launch_k(blocks > 0, sh_qk_norm_gain_kernel, dim3((unsigned)((p.d_head + 31) / 32), 2), dim3(32, 32), 0, st, g);
   }
   return SH_OK;
@@ -198,10 +186,13 @@ struct BlPlan { int w, l, per, ny, tpb, nx; bool vec; };
 constexpr size_t kBlHead = 256;
 size_t bl_losses(long long gates) { return ((size_t)gates * 8 + 255) / 256 * 256; }
 
+// Logits of a lane: 32 bytes of them, fewer where there are no more.
+int bl_width(int dtype, int E) { return E <= 4 ? 4 : E <= 8 || dtype == SH_F32 ? 8 : 16; }
+
 // The thread layout for E logits of a gate; `vec`: rows are whole, aligned vectors.
 BlPlan bl_plan(int dtype, long long tokens, int gates, int E, bool aligned, int sms) {
   BlPlan p;
-  p.w = dtype == SH_F32 || E <= 4 ? 4 : 8;
+  p.w = bl_width(dtype, E);
   p.l = pow2_at_least((E + p.w - 1) / p.w);
   p.vec = aligned && E == p.w * p.l;
   const int rows = BL_THREADS / p.l;
@@ -209,14 +200,15 @@ BlPlan bl_plan(int dtype, long long tokens, int gates, int E, bool aligned, int 
   p.per = (gates + p.ny - 1) / p.ny;
   p.tpb = rows / p.per;
   const long long rounds = (tokens + p.tpb - 1) / p.tpb;
-  long long cap = 4ll * sms < BL_MAX_BLOCKS ? 4ll * sms : BL_MAX_BLOCKS;
+  long long cap = 3ll * sms < BL_MAX_BLOCKS ? 3ll * sms : BL_MAX_BLOCKS;
   cap = cap / p.ny < 1 ? 1 : cap / p.ny;
-  p.nx = (int)(rounds < 1 ? 1 : rounds < cap ? rounds : cap);
+  const long long turns = (rounds + 1) / 2;                // (two rows of a thread at least are on their way together)
+  p.nx = (int)(turns < 1 ? 1 : turns < cap ? turns : cap);
   return p;
 }
 
 bool bl_aligned(const void* z, long long stride, int gates, int E, int w, int size, long long tokens) {
-  const size_t bytes = (size_t)w * size;
+  const size_t bytes = (size_t)w * size < 16 ? (size_t)w * size : 16;
   return (uintptr_t)z % bytes == 0 && (tokens < 2 || (size_t)stride * size % bytes == 0) && (gates < 2 || (size_t)E * size % bytes == 0);
 }
 
@@ -270,20 +262,20 @@ int bl_launch(const BlArgs& a, const BlPlan& p, int what, bool pdl, cudaStream_t
 int bl_dispatch(int dtype, const BlArgs& a, const BlPlan& p, int what, bool pdl, cudaStream_t st) {
 #define SH_BL(T, W, L) return p.vec ? bl_launch<T, W, L, true>(a, p, what, pdl, st) : bl_launch<T, W, L, false>(a, p, what, pdl, st)
   if (dtype == SH_F32) {
-    if (p.l == 1) SH_BL(float, 4, 1);
-    if (p.l == 2) SH_BL(float, 4, 2);
-    if (p.l == 4) SH_BL(float, 4, 4);
-    SH_BL(float, 4, 8);
+    if (p.w == 4) SH_BL(float, 4, 1);
+    if (p.l == 1) SH_BL(float, 8, 1);
+    if (p.l == 2) SH_BL(float, 8, 2);
+    SH_BL(float, 8, 4);
   }
   if (p.w == 4) SH_BL(__nv_bfloat16, 4, 1);
-  if (p.l == 1) SH_BL(__nv_bfloat16, 8, 1);
-  if (p.l == 2) SH_BL(__nv_bfloat16, 8, 2);
-  SH_BL(__nv_bfloat16, 8, 4);
+  if (p.w == 8) SH_BL(__nv_bfloat16, 8, 1);
+  if (p.l == 1) SH_BL(__nv_bfloat16, 16, 1);
+  SH_BL(__nv_bfloat16, 16, 2);
 #undef SH_BL
 }
 
 BlPlan bl_plan_for(const sh_balance_args& p, bool backward, int sms) {
-  const int gates = p.sides * p.n_heads, size = (int)elem_bytes(p.dtype), w = p.dtype == SH_F32 || p.n_experts <= 4 ? 4 : 8;
+  const int gates = p.sides * p.n_heads, size = (int)elem_bytes(p.dtype), w = bl_width(p.dtype, p.n_experts);
   bool aligned = bl_aligned(p.logits, p.token_stride, gates, p.n_experts, w, size, p.n_tokens);
   if (backward) aligned = aligned && bl_aligned(p.dlogits, p.dtoken_stride, gates, p.n_experts, w, size, p.n_tokens);
   return bl_plan(p.dtype, p.n_tokens, gates, p.n_experts, aligned, sms);
@@ -292,24 +284,28 @@ BlPlan bl_plan_for(const sh_balance_args& p, bool backward, int sms) {
 }  // namespace
 
 extern "C" int sh_qk_norm(const sh_qk_norm_args* args, void* stream) {
-  if (int rc = qn_check(args, false)) return rc;
+  sh_set_error("%s", "");
+  if (!args) { sh_set_error("args is NULL"); return SH_ERR_INVALID_ARG; }
+  if (int rc = qn_check(*args, nullptr)) return rc;
   if (args->batch == 0 || args->seq == 0) return SH_OK;
-  return qn_run(*args, false, false, (cudaStream_t)stream);
+  return qn_run(*args, nullptr, false, (cudaStream_t)stream);
 }
 
 extern "C" size_t sh_qk_norm_workspace_bytes(int d_head) {
   return d_head < 1 || d_head > QN_MAX_D ? 0 : (size_t)QN_MAX_BLOCKS * d_head * 4;
 }
 
-extern "C" int sh_qk_norm_backward(const sh_qk_norm_args* args, void* stream) {
-  if (int rc = qn_check(args, true)) return rc;
-  const sh_qk_norm_args& a = *args;
-  const size_t need = sh_qk_norm_workspace_bytes(a.d_head);
+extern "C" int sh_qk_norm_backward(const sh_qk_norm_backward_args* args, void* stream) {
+  sh_set_error("%s", "");
+  if (!args) { sh_set_error("args is NULL"); return SH_ERR_INVALID_ARG; }
+  const sh_qk_norm_backward_args& a = *args;
+  if (int rc = qn_check(a.norm, args)) return rc;
   if (a.dgq || a.dgk) {
+    const size_t need = sh_qk_norm_workspace_bytes(a.norm.d_head);
     if (!a.workspace || (uintptr_t)a.workspace % 256) { sh_set_error("workspace must be a device pointer aligned to 256 bytes"); return SH_ERR_WORKSPACE; }
     if (a.workspace_bytes < need) { sh_set_error("workspace too small: %zu bytes given, %zu needed", a.workspace_bytes, need); return SH_ERR_WORKSPACE; }
   }
-  return qn_run(a, true, false, (cudaStream_t)stream);
+  return qn_run(a.norm, args, false, (cudaStream_t)stream);
 }
 
 extern "C" size_t sh_balance_workspace_bytes(int sides, int n_heads, int n_experts) {
@@ -337,7 +333,7 @@ extern "C" int sh_balance_loss(const sh_balance_args* args, void* stream) {
   o.part_p = a.part_p; o.part_n = a.part_n; o.ticket = a.ticket; o.gate_loss = (double*)(ws + kBlHead);
   o.blocks = pl.nx; o.gates = a.gates; o.E = a.E; o.kind = p.kind; o.coef = p.coef;
   o.loss = p.loss; o.prob = p.prob; o.slope = p.slope; o.counts = p.counts;
-  return launch_k(true, sh_balance_loss_kernel, dim3((unsigned)a.gates), dim3(BL_THREADS), 0, st, o);
+  return launch_k(true, sh_balance_loss_kernel, dim3((unsigned)a.gates), dim3(BL_LOSS_THREADS), 0, st, o);
 }
 
 extern "C" int sh_balance_backward(const sh_balance_args* args, void* stream) {

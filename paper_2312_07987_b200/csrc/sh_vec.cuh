@@ -1,34 +1,41 @@
-// Vectors of V stored values as fp32 in registers: loads, stores, conversions of the streaming kernels.
+// Vectors of V stored values: held as loaded (what is on its way costs few registers), turned into fp32, stored.
 #pragma once
 #include "sh_internal.cuh"
 
-// V values of T from p (aligned to V values) to fp32.  ONCE: what no other thread reads goes past L1.
-template <typename T, int V, bool ONCE = true>
-__device__ __forceinline__ void sh_load(const T* p, float (&f)[V]) {
-  constexpr int BYTES = V * (int)sizeof(T);
-  if constexpr (BYTES >= 4) {
-    uint32_t w[BYTES / 4];
+template <typename T, int V>
+struct ShRaw {
+  static constexpr int BYTES = V * (int)sizeof(T);
+  uint32_t w[BYTES < 4 ? 1 : BYTES / 4];
+
+  // (aligned to V values; evict-first: nobody reads it again)
+  __device__ __forceinline__ void load(const T* p) {
     if constexpr (BYTES >= 16) {
 #pragma unroll
       for (int i = 0; i < BYTES / 16; ++i) {
-        const uint4 v = ONCE ? __ldcs(reinterpret_cast<const uint4*>(p) + i) : __ldg(reinterpret_cast<const uint4*>(p) + i);
+        const uint4 v = __ldcs(reinterpret_cast<const uint4*>(p) + i);
         w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
       }
     } else if constexpr (BYTES == 8) {
-      const uint2 v = ONCE ? __ldcs(reinterpret_cast<const uint2*>(p)) : __ldg(reinterpret_cast<const uint2*>(p));
+      const uint2 v = __ldcs(reinterpret_cast<const uint2*>(p));
       w[0] = v.x; w[1] = v.y;
+    } else if constexpr (BYTES == 4) {
+      w[0] = __ldcs(reinterpret_cast<const uint32_t*>(p));
     } else {
-      w[0] = ONCE ? __ldcs(reinterpret_cast<const uint32_t*>(p)) : __ldg(reinterpret_cast<const uint32_t*>(p));
+      w[0] = __ldcs(reinterpret_cast<const unsigned short*>(p));
     }
+  }
+  __device__ __forceinline__ void fill(uint32_t word) {
+#pragma unroll
+    for (int i = 0; i < (BYTES < 4 ? 1 : BYTES / 4); ++i) w[i] = word;
+  }
+  __device__ __forceinline__ void get(float (&f)[V]) const {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       if constexpr (sizeof(T) == 4) f[i] = __uint_as_float(w[i]);
       else f[i] = sh_to_float<T>(reinterpret_cast<const T*>(w)[i]);
     }
-  } else {
-    f[0] = sh_to_float<T>(p[0]);
   }
-}
+};
 
 template <typename T, int V>
 __device__ __forceinline__ void sh_store(T* p, const float (&f)[V]) {

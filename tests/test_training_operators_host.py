@@ -5,45 +5,50 @@ import torch
 
 from paper_2312_07987_b200 import binding as b
 
-HEADS = ("data", "batch_stride", "token_stride", "head_stride", "heads", "reserved")
-NORM = ("gq", "gk", "dgq", "dgk", "positions", "workspace", "workspace_bytes", "base", "dtype", "batch", "seq", "d_head", "rotated", "halves", "positions_64", "eps", "q_scale", "reserved")
+HEADS = ("data", "batch_stride", "token_stride", "head_stride")
+NORM = ("gq", "gk", "positions", "base", "dtype", "batch", "seq", "q_heads", "k_heads", "d_head", "rotated", "halves", "positions_64", "eps", "q_scale", "reserved")
+BACKWARD = ("dgq", "dgk", "workspace", "workspace_bytes")
 BALANCE = ("n_tokens", "token_stride", "dtoken_stride", "logits", "idx", "mask", "gloss", "loss", "prob", "slope", "counts", "dlogits", "workspace", "workspace_bytes",
            "dtype", "kind", "sides", "n_heads", "n_experts", "k", "coef", "reserved")
 DROPOUT = ("x", "residual", "y", "rng", "rows", "cols", "x_stride", "residual_stride", "y_stride", "p", "dtype", "reserved")
 PTR = 0x1000          # never used as an address: each call below is refused
 
 
-def norm_args(heads=None, **kw):
-    h = {n: dict(data=PTR, batch_stride=256, token_stride=64, head_stride=32, heads=2, reserved=0) for n in ("q", "k", "q_out", "k_out", "dq", "dk")}
+def norm_args(heads=None, backward=False, **kw):
+    h = {n: dict(data=PTR, batch_stride=256, token_stride=64, head_stride=32) for n in ("q", "k", "q_out", "k_out", "dq", "dk")}
     for n, v in (heads or {}).items():
         h[n].update(v)
-    f = dict(gq=0, gk=0, dgq=0, dgk=0, positions=0, workspace=0, workspace_bytes=0, base=10000.0, dtype=b.SH_F32, batch=2, seq=4, d_head=32, rotated=32, halves=0,
-             positions_64=0, eps=1e-6, q_scale=1.0, reserved=0)
+    f = dict(gq=0, gk=0, dgq=0, dgk=0, positions=0, workspace=0, workspace_bytes=0, base=10000.0, dtype=b.SH_F32, batch=2, seq=4, q_heads=2, k_heads=2, d_head=32, rotated=32,
+             halves=0, positions_64=0, eps=1e-6, q_scale=1.0, reserved=0)
     f.update(kw)
-    return b._QK_NORM.pack(*[h[n][m] for n in h for m in HEADS], *[f[n] for n in NORM])
+    fields = [h[n][m] for n in list(h)[:4] for m in HEADS] + [f[n] for n in NORM]
+    if not backward:
+        return b._QK_NORM.pack(*fields)
+    return b._QK_NORM_BACKWARD.pack(*fields, *[h[n][m] for n in ("dq", "dk") for m in HEADS], *[f[n] for n in BACKWARD])
 
 
 @pytest.mark.parametrize("kw,heads,code,frag", [
     (dict(dtype=3), {}, -1, "dtype"), (dict(batch=-1), {}, -1, "batch"), (dict(seq=-1), {}, -1, "seq"), (dict(d_head=0), {}, -1, "d_head"),
     (dict(d_head=257), {}, -1, "d_head"), (dict(rotated=3), {}, -1, "rotated"), (dict(rotated=34), {}, -1, "rotated"), (dict(rotated=-2), {}, -1, "rotated"),
     (dict(d_head=33, rotated=32), {}, -2, "even d_head"), (dict(base=0.0), {}, -1, "base"), (dict(base=float("nan")), {}, -1, "base"), (dict(eps=0.0), {}, -1, "eps"),
-    (dict(eps=float("nan")), {}, -1, "eps"), (dict(q_scale=float("inf")), {}, -1, "q_scale"), ({}, dict(q=dict(heads=-1)), -1, "heads"), ({}, dict(k=dict(data=0)), -1, "k: data"),
+    (dict(eps=float("nan")), {}, -1, "eps"), (dict(q_scale=float("inf")), {}, -1, "q_scale"), (dict(q_heads=-1), {}, -1, "heads"), ({}, dict(k=dict(data=0)), -1, "k and k_out"),
     ({}, dict(q_out=dict(data=0)), -1, "q_out"), ({}, dict(k_out=dict(token_stride=0)), -1, "share an address"), ({}, dict(q_out=dict(head_stride=0)), -1, "share an address"),
+    ({}, dict(q=dict(data=PTR + 2)), -1, "not aligned"),
 ])
 def test_norm_refusals(kw, heads, code, frag):
-    for fn in (b.lib.sh_qk_norm, b.lib.sh_qk_norm_backward):
-        assert fn(norm_args(heads, **kw), None) == code
+    for fn, backward in ((b.lib.sh_qk_norm, False), (b.lib.sh_qk_norm_backward, True)):
+        assert fn(norm_args(heads, backward, **kw), None) == code
         assert frag in b.sh_last_error()
 
 
 def test_norm_backward_refusals():
     fn = b.lib.sh_qk_norm_backward
-    assert fn(norm_args(dict(dq=dict(data=0))), None) == -1 and "dq" in b.sh_last_error()
-    assert fn(norm_args(dgq=PTR), None) == -4 and "workspace" in b.sh_last_error()
+    assert fn(norm_args(dict(dq=dict(data=0)), True), None) == -1 and "dq" in b.sh_last_error()
+    assert fn(norm_args(None, True, dgq=PTR), None) == -4 and "workspace" in b.sh_last_error()
     need = b.lib.sh_qk_norm_workspace_bytes(32)
     assert need > 0 and b.lib.sh_qk_norm_workspace_bytes(0) == 0 and b.lib.sh_qk_norm_workspace_bytes(257) == 0
-    assert fn(norm_args(dgq=PTR, workspace=PTR + 8, workspace_bytes=need), None) == -4
-    assert fn(norm_args(dgk=PTR, workspace=PTR, workspace_bytes=need - 1), None) == -4 and "too small" in b.sh_last_error()
+    assert fn(norm_args(None, True, dgq=PTR, workspace=PTR + 8, workspace_bytes=need), None) == -4
+    assert fn(norm_args(None, True, dgk=PTR, workspace=PTR, workspace_bytes=need - 1), None) == -4 and "too small" in b.sh_last_error()
     for f in (b.lib.sh_qk_norm, fn, b.lib.sh_balance_loss, b.lib.sh_balance_backward, b.lib.sh_dropout):
         assert f(None, None) == -1 and "NULL" in b.sh_last_error()
 
