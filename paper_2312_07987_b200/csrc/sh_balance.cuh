@@ -172,12 +172,19 @@ static __global__ void __launch_bounds__(BL_LOSS_THREADS) sh_balance_loss_kernel
   const int gate = blockIdx.x, e = threadIdx.x & 31, r = threadIdx.x >> 5, cols = a.gates * a.E;
   double p = 0.0;
   int n = 0, tokens = 0;
-  if (e < a.E)
-#pragma unroll 16
-    for (int b = r; b < a.blocks; b += ROWS) {
-      p += (double)__ldcg(a.part_p + (long long)b * cols + gate * a.E + e);
-      n += __ldcg(a.part_n + (long long)b * cols + gate * a.E + e);
+  for (int b = r; b < a.blocks; b += 16 * ROWS) {
+    float vp[16];                                        // (loads of a round in flight together)
+    int vn[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const bool there = e < a.E && b + k * ROWS < a.blocks;
+      const long long at = (long long)(b + k * ROWS) * cols + gate * a.E + e;
+      vp[k] = there ? __ldcg(a.part_p + at) : 0.f;
+      vn[k] = there ? __ldcg(a.part_n + at) : 0;
     }
+#pragma unroll
+    for (int k = 0; k < 16; ++k) { p += (double)vp[k]; n += vn[k]; }
+  }
   for (int b = threadIdx.x; b < a.blocks; b += BL_LOSS_THREADS) tokens += __ldcg(a.part_n + (long long)a.blocks * cols + b);
   s_p[r][e] = p; s_n[r][e] = n;
   for (int o = 16; o > 0; o >>= 1) tokens += __shfl_xor_sync(0xffffffffu, tokens, o);

@@ -2,7 +2,7 @@
 //
 //   r = (mean(x^2) + eps)^-1/2,  y = s Rot(pos) (g x r);   u = s Rot(-pos) dy,  dg = sum u x r,  dx = r (g u - x r mean(g u x r))
 //
-// A row (one token's head) belongs to `lanes` neighbouring lanes with NV vectors of V values each, in registers from the
+// A row (one token's head) belongs to LANES neighbouring lanes with NV vectors of V values each, in registers from the
 // load to the store: x is read once and y written once, the mean is a butterfly over the group.  A pair of rotated columns
 // never leaves its lane: neighbouring columns lie in one vector, columns half the rotated width apart in two vectors of the
 // same lane.  A group takes several heads of one token, which share the angles.
@@ -15,6 +15,10 @@
 constexpr int QN_THREADS = 256;
 
 constexpr int QN_MAX_D = 256;
+// The backward kernel's vectors are of 4 values at most (8 of a 16-bit type: 128 registers and spills; 33.5 M values of 16384 tokens, 16 heads
+// of 128: 56 us, with 4 44), and its blocks 3 to an SM (fp32, whose rows on their way are twice as large: 2; 8 x 256 tokens: 13.5 us with 3, 9.0).
+constexpr int QN_BACKWARD_V = 4;
+template <typename T> __host__ __device__ constexpr int qn_backward_blocks() { return sizeof(T) == 4 ? 2 : 3; }
 constexpr int QN_MAX_BLOCKS = 1024;       // blocks of the backward kernel at most (rows of its partial gain gradients)
 
 struct QnSide {
@@ -30,7 +34,7 @@ struct QnArgs {
   const void* pos;                                       // [batch, seq] or nullptr: the token's place in its sequence
   int pos64, next;                                       // next: rotated pairs are neighbouring columns
   int seq, D, R;                                         // R: rotated columns
-  int lanes, per;                                        // lanes to a row; heads to a group
+  int per;                                               // heads to a group
   long long tokens;                                      // batch * seq
   int blocks0;                                           // backward: blocks of the queries (the rest: keys)
   float eps;
@@ -38,22 +42,22 @@ struct QnArgs {
   unsigned long long freq[QN_MAX_D / 2];                 // turns per position of each pair, times 2^64
 };
 
-// The columns of a lane's vectors (-1: none): vector i at (lane + i lanes) V, with neighbouring pairs inside a vector; or,
+// The columns of a lane's vectors (-1: none): vector i at (lane + i LANES) V, with neighbouring pairs inside a vector; or,
 // PAIRED, vectors 2 j and 2 j + 1 in the two halves of the rotated columns, or of the columns behind them.  (Vectors of one
 // value, where the addresses allow no more, are paired in either order.)
-template <int V, int NV, bool PAIRED>
+template <int V, int NV, int LANES, bool PAIRED>
 __device__ __forceinline__ void qn_columns(const QnArgs& a, int l, int (&col)[NV]) {
   if constexpr (!PAIRED) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (l + i * a.lanes) * V;
+      const int c = (l + i * LANES) * V;
       col[i] = c < a.D ? c : -1;
     }
   } else {
     const int h = a.R / 2, t = (a.D - a.R) / 2;
 #pragma unroll
     for (int j = 0; j < NV / 2; ++j) {
-      const int p = (l + j * a.lanes) * V;
+      const int p = (l + j * LANES) * V;
       if (V == 1 && a.next) {
         col[2 * j] = 2 * p < a.D ? 2 * p : -1;
         col[2 * j + 1] = 2 * p < a.D ? 2 * p + 1 : -1;
@@ -64,6 +68,12 @@ __device__ __forceinline__ void qn_columns(const QnArgs& a, int l, int (&col)[NV
       col[2 * j + 1] = rot ? h + p : tail ? a.R + t + p - h : -1;
     }
   }
+}
+
+// Vector i of a row whose lane's first vector is at p.  (Without pairs the distance is known to the compiler.)
+template <int V, int NV, int LANES, bool PAIRED, typename T>
+__device__ __forceinline__ T* qn_vector(T* p, const int (&col)[NV], int i) {
+  return p + (PAIRED ? col[i] - col[0] : i * LANES * V);
 }
 
 // The lane's values as pairs (A, B) that a rotation mixes, two pairs to a register pair (packed fp32 arithmetic: two
@@ -88,8 +98,8 @@ __device__ __forceinline__ void qn_get(const ShRaw<T, V> (&raw)[NV], QnPairs<NV 
     qn_half(x.b[n / 2], n & 1) = f[qn_vec_b<V, PAIRED>(n)][qn_at_b<V, PAIRED>(n)];
   }
 }
-template <typename T, int V, int NV, bool PAIRED>
-__device__ __forceinline__ void qn_put(T* const (&p)[NV], const int (&col)[NV], QnPairs<NV * V / 2>& x) {
+template <typename T, int V, int NV, int LANES, bool PAIRED>
+__device__ __forceinline__ void qn_put(T* p, const int (&col)[NV], QnPairs<NV * V / 2>& x) {
   float f[NV][V];
 #pragma unroll
   for (int n = 0; n < NV * V / 2; ++n) {
@@ -98,7 +108,19 @@ __device__ __forceinline__ void qn_put(T* const (&p)[NV], const int (&col)[NV], 
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i)
-    if (col[i] >= 0) sh_store<T, V>(p[i], f[i]);
+    if (col[i] >= 0) sh_store<T, V>(qn_vector<V, NV, LANES, PAIRED>(p, col, i), f[i]);
+}
+
+// The lane's gains: ones where there are none.
+template <int V, int NV, bool PAIRED>
+__device__ __forceinline__ void qn_gains(const float* gain, const int (&col)[NV], QnPairs<NV * V / 2>& g) {
+  ShRaw<float, V> raw[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    raw[i].fill(0x3F800000u);
+    if (gain && col[i] >= 0) raw[i].load(gain + col[i]);
+  }
+  qn_get<float, V, NV, PAIRED>(raw, g);
 }
 
 // cos and sin of pair n at a position: 1 and 0 behind the rotated columns.  16-bit results: the special function unit's (off by
@@ -110,8 +132,9 @@ __device__ __forceinline__ void qn_angle(const QnArgs& a, const unsigned long lo
   const int pair = next ? at / 2 : at;
   *cs = 1.f; *sn = 0.f;
   if (c >= 0 && pair < a.R / 2) {
-    const unsigned long long turns = (unsigned long long)pos * freq[pair];
-    const float x = (float)(int)(turns >> 32);           // half turns times 2^31
+    const unsigned long long f = freq[pair];
+    // (the upper half of the product's lower 64 bits: half turns times 2^31)
+    const float x = (float)(int)(__umulhi((unsigned)pos, (unsigned)f) + (unsigned)pos * (unsigned)(f >> 32) + (unsigned)(pos >> 32) * (unsigned)f);
     if constexpr (sizeof(T) == 2) __sincosf(x * (3.14159265f * 4.656612873077393e-10f), sn, cs);
     else sincospif(x * 4.656612873077393e-10f, sn, cs);
   }
@@ -124,15 +147,14 @@ __device__ __forceinline__ long long qn_position(const QnArgs& a, long long toke
 __device__ __forceinline__ long long qn_div(long long n, int d) { return n >> 32 ? n / d : (long long)((unsigned)n / (unsigned)d); }
 
 // V = 1 without pairs: nothing is rotated (d_head may be odd).
-template <typename T, int V, int NV, bool PAIRED>
+template <typename T, int V, int NV, int LANES, bool PAIRED>
 static __global__ void __launch_bounds__(QN_THREADS, 3) sh_qk_norm_kernel(const __grid_constant__ QnArgs a) {
   __shared__ unsigned long long s_freq[QN_MAX_D / 2];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   constexpr int P = NV * V / 2;
   for (int i = threadIdx.x; i < a.R / 2; i += QN_THREADS) s_freq[i] = a.freq[i];
-  if (a.R) __syncthreads();
-  const int l = threadIdx.x & (a.lanes - 1);
-  const long long item = (long long)blockIdx.x * (QN_THREADS / a.lanes) + threadIdx.x / a.lanes;
+  const int l = threadIdx.x % LANES;
+  const long long item = (long long)blockIdx.x * (QN_THREADS / LANES) + threadIdx.x / LANES;
   const int chunks = a.s[0].chunks + a.s[1].chunks;
   const long long token = qn_div(item, chunks);
   const bool live = token < a.tokens;                    // (a warp's groups shuffle together: none leaves early)
@@ -144,35 +166,35 @@ static __global__ void __launch_bounds__(QN_THREADS, 3) sh_qk_norm_kernel(const 
   const int t = (int)(token - b * a.seq);
   const int h0 = chunk * a.per, n = live ? min(a.per, s.heads - h0) : 0;
   int col[NV];
-  qn_columns<V, NV, PAIRED>(a, l, col);
-  const T* px[NV];
-  T* py[NV];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    px[i] = (const T*)s.x + b * s.xb + t * s.xt + h0 * s.xh + col[i];
-    py[i] = (T*)s.out + b * s.ob + t * s.ot + h0 * s.oh + col[i];
-  }
-  // the next two heads' values are on their way while one is worked on; the same number of rounds for every group of a warp
+  qn_columns<V, NV, LANES, PAIRED>(a, l, col);
+  const T* px = (const T*)s.x + b * s.xb + t * s.xt + h0 * s.xh + col[0];
+  T* py = (T*)s.out + b * s.ob + t * s.ot + h0 * s.oh + col[0];
+  // The next two heads' values are on their way while one is worked on; the same number of rounds for every group of a warp.
+  // (A lane without columns keeps its zeros, a group without a next head what it has: it is not stored.)
   ShRaw<T, V> raw[2][NV];
-  auto fetch = [&](int j) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      if (j < n && col[i] >= 0) raw[j & 1][i].load(px[i]);
-      else raw[j & 1][i].fill(0);
-      px[i] += s.xh;
+  for (int i = 0; i < NV; ++i) { raw[0][i].fill(0); raw[1][i].fill(0); }
+  auto fetch = [&](int j, ShRaw<T, V> (&to)[NV]) {
+    if (j < n) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (col[i] >= 0) to[i].load(qn_vector<V, NV, LANES, PAIRED>(px, col, i));
     }
+    px += s.xh;
   };
-  fetch(0); fetch(1);
+  fetch(0, raw[0]); fetch(1, raw[1]);
+  const long long pos = live && a.R ? qn_position(a, token, t) : 0;
+  QnPairs<P> g;
+  qn_gains<V, NV, PAIRED>(s.gain, col, g);
+  if (a.R) __syncthreads();                              // the frequencies
   // y = r (A ga cs - B gb sn, A ga sn + B gb cs): gains, scale and angles in four factors a pair, for all of the heads
   QnPairs<P> fa, fb;
 #pragma unroll
   for (int m = 0; m < P; ++m) {
     float cs = 1.f, sn = 0.f;
     if constexpr (V > 1 || PAIRED)
-      if (a.R && live) qn_angle<T, V, NV, PAIRED>(a, s_freq, qn_position(a, token, t), col, m, &cs, &sn);
-    const int ca = col[qn_vec_a<V, PAIRED>(m)], cb = col[qn_vec_b<V, PAIRED>(m)];
-    const float ga = s.scale * (s.gain && ca >= 0 ? __ldg(s.gain + ca + qn_at_a<V, PAIRED>(m)) : 1.f);
-    const float gb = s.scale * (s.gain && cb >= 0 ? __ldg(s.gain + cb + qn_at_b<V, PAIRED>(m)) : 1.f);
+      if (a.R) qn_angle<T, V, NV, PAIRED>(a, s_freq, pos, col, m, &cs, &sn);
+    const float ga = s.scale * qn_half(g.a[m / 2], m & 1), gb = s.scale * qn_half(g.b[m / 2], m & 1);
     qn_half(fa.a[m / 2], m & 1) = ga * cs; qn_half(fa.b[m / 2], m & 1) = -gb * sn;
     qn_half(fb.a[m / 2], m & 1) = ga * sn; qn_half(fb.b[m / 2], m & 1) = gb * cs;
   }
@@ -180,11 +202,9 @@ static __global__ void __launch_bounds__(QN_THREADS, 3) sh_qk_norm_kernel(const 
   for (int j0 = 0; j0 < a.per; j0 += 2) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int j = j0 + u;
-      if (j >= a.per) break;
       QnPairs<P> x, y;
       qn_get<T, V, NV, PAIRED>(raw[u], x);
-      fetch(j0 + 2 + u);
+      fetch(j0 + u + 2, raw[u]);
       float2 ss = make_float2(0.f, 0.f);
 #pragma unroll
       for (int m = 0; m < P / 2; ++m) {
@@ -193,13 +213,12 @@ static __global__ void __launch_bounds__(QN_THREADS, 3) sh_qk_norm_kernel(const 
         y.a[m] = __ffma2_rn(x.a[m], fa.a[m], __fmul2_rn(x.b[m], fa.b[m]));
         y.b[m] = __ffma2_rn(x.a[m], fb.a[m], __fmul2_rn(x.b[m], fb.b[m]));
       }
-      const float r = rsqrtf(fmaf(sh_group_sum(ss.x + ss.y, a.lanes), inv, a.eps));
+      const float r = rsqrtf(fmaf(sh_group_sum<LANES>(ss.x + ss.y), inv, a.eps));
       const float2 rr = make_float2(r, r);
 #pragma unroll
       for (int m = 0; m < P / 2; ++m) { y.a[m] = __fmul2_rn(y.a[m], rr); y.b[m] = __fmul2_rn(y.b[m], rr); }
-      if (j < n) qn_put<T, V, NV, PAIRED>(py, col, y);
-#pragma unroll
-      for (int i = 0; i < NV; ++i) py[i] += s.oh;
+      if (j0 + u < n) qn_put<T, V, NV, LANES, PAIRED>(py, col, y);
+      py += s.oh;
     }
   }
 }
@@ -207,99 +226,100 @@ static __global__ void __launch_bounds__(QN_THREADS, 3) sh_qk_norm_kernel(const 
 // The first `blocks0` blocks take the queries, the others the keys, each in rounds over its side's (token, chunk of heads).
 // A thread adds its columns' share of the gain gradients over its rows; the block's groups are added in order in shared
 // memory, the blocks by sh_qk_norm_gain_kernel: the same bits on every run.
-template <typename T, int V, int NV, bool PAIRED>
-static __global__ void __launch_bounds__(QN_THREADS, 2) sh_qk_norm_backward_kernel(const __grid_constant__ QnArgs a) {
+template <typename T, int V, int NV, int LANES, bool PAIRED>
+static __global__ void __launch_bounds__(QN_THREADS, qn_backward_blocks<T>()) sh_qk_norm_backward_kernel(const __grid_constant__ QnArgs a) {
   __shared__ unsigned long long s_freq[QN_MAX_D / 2];
   extern __shared__ float s_sum[];                       // [groups][D]
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  constexpr int P = NV * V / 2;
+  constexpr int P = NV * V / 2, GROUPS = QN_THREADS / LANES;
   for (int i = threadIdx.x; i < a.R / 2; i += QN_THREADS) s_freq[i] = a.freq[i];
   if (a.R) __syncthreads();
-  const int l = threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes, groups = QN_THREADS / a.lanes;
+  const int l = threadIdx.x % LANES, group = threadIdx.x / LANES;
   const int side = (int)blockIdx.x >= a.blocks0;
   const QnSide& s = a.s[side];
   const int block = side ? blockIdx.x - a.blocks0 : blockIdx.x, blocks = side ? gridDim.x - a.blocks0 : a.blocks0;
   int col[NV];
-  qn_columns<V, NV, PAIRED>(a, l, col);
+  qn_columns<V, NV, LANES, PAIRED>(a, l, col);
   QnPairs<P> g, dg;
+  qn_gains<V, NV, PAIRED>(s.gain, col, g);
 #pragma unroll
-  for (int m = 0; m < P; ++m) {
-    const int ca = col[qn_vec_a<V, PAIRED>(m)], cb = col[qn_vec_b<V, PAIRED>(m)];
-    qn_half(g.a[m / 2], m & 1) = s.gain && ca >= 0 ? __ldg(s.gain + ca + qn_at_a<V, PAIRED>(m)) : 1.f;
-    qn_half(g.b[m / 2], m & 1) = s.gain && cb >= 0 ? __ldg(s.gain + cb + qn_at_b<V, PAIRED>(m)) : 1.f;
-    qn_half(dg.a[m / 2], m & 1) = qn_half(dg.b[m / 2], m & 1) = 0.f;
-  }
+  for (int m = 0; m < P / 2; ++m) dg.a[m] = dg.b[m] = make_float2(0.f, 0.f);
   const float inv = 1.f / (float)a.D;
-  const long long items = a.tokens * s.chunks, step = (long long)blocks * groups;
+  const long long items = a.tokens * s.chunks, step = (long long)blocks * GROUPS;
   // (rounds: the same for every group of the block)
-  for (long long first = (long long)block * groups; first < items; first += step) {
+  for (long long first = (long long)block * GROUPS; first < items; first += step) {
     const long long item = first + group;
     const bool live = item < items;
     const long long token = live ? qn_div(item, s.chunks) : 0;
     const int h0 = live ? (int)(item - token * s.chunks) * a.per : 0, n = live ? min(a.per, s.heads - h0) : 0;
     const long long b = qn_div(token, a.seq);
     const int t = (int)(token - b * a.seq);
-    const T *px[NV], *py[NV];
-    T* po[NV];
+    const T* px = (const T*)s.x + b * s.xb + t * s.xt + h0 * s.xh + col[0];
+    const T* pd = (const T*)s.dy + b * s.yb + t * s.yt + h0 * s.yh + col[0];
+    T* po = (T*)s.out + b * s.ob + t * s.ot + h0 * s.oh + col[0];
+    // (as in the forward pass: the next two heads' values on their way)
+    ShRaw<T, V> rx[2][NV], ry[2][NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      px[i] = (const T*)s.x + b * s.xb + t * s.xt + h0 * s.xh + col[i];
-      py[i] = (const T*)s.dy + b * s.yb + t * s.yt + h0 * s.yh + col[i];
-      po[i] = (T*)s.out + b * s.ob + t * s.ot + h0 * s.oh + col[i];
-    }
-    // the next head's values are on their way while one is worked on
-    ShRaw<T, V> rx[NV], ry[NV];
-    auto fetch = [&](int j) {
+    for (int i = 0; i < NV; ++i) { rx[0][i].fill(0); rx[1][i].fill(0); ry[0][i].fill(0); ry[1][i].fill(0); }
+    auto fetch = [&](int j, ShRaw<T, V> (&x)[NV], ShRaw<T, V> (&y)[NV]) {
+      if (j < n) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        if (j < n && col[i] >= 0) { rx[i].load(px[i]); ry[i].load(py[i]); }
-        else { rx[i].fill(0); ry[i].fill(0); }
-        px[i] += s.xh; py[i] += s.yh;
+        for (int i = 0; i < NV; ++i)
+          if (col[i] >= 0) {
+            x[i].load(qn_vector<V, NV, LANES, PAIRED>(px, col, i));
+            y[i].load(qn_vector<V, NV, LANES, PAIRED>(pd, col, i));
+          }
       }
+      px += s.xh; pd += s.yh;
     };
-    fetch(0);
+    fetch(0, rx[0], ry[0]); fetch(1, rx[1], ry[1]);
+    const long long pos = live && a.R ? qn_position(a, token, t) : 0;
     float2 cs[P / 2], sn[P / 2];                         // times the scale
 #pragma unroll
     for (int m = 0; m < P; ++m) {
       float c = 1.f, d = 0.f;
       if constexpr (V > 1 || PAIRED)
-        if (a.R && live) qn_angle<T, V, NV, PAIRED>(a, s_freq, qn_position(a, token, t), col, m, &c, &d);
+        if (a.R) qn_angle<T, V, NV, PAIRED>(a, s_freq, pos, col, m, &c, &d);
       qn_half(cs[m / 2], m & 1) = s.scale * c; qn_half(sn[m / 2], m & 1) = s.scale * d;
     }
-    for (int j = 0; j < a.per; ++j) {
-      QnPairs<P> x, y, u;
-      qn_get<T, V, NV, PAIRED>(rx, x);
-      qn_get<T, V, NV, PAIRED>(ry, y);
-      fetch(j + 1);
-      // u = s Rot(-pos) dy;  t = u x;  sums of x^2 and of g t;  dx = r (g u) - r m x
-      float2 ss = make_float2(0.f, 0.f), wx = ss;
+    for (int j0 = 0; j0 < a.per; j0 += 2) {
 #pragma unroll
-      for (int m = 0; m < P / 2; ++m) {
-        u.a[m] = __ffma2_rn(y.a[m], cs[m], __fmul2_rn(y.b[m], sn[m]));
-        u.b[m] = __ffma2_rn(y.b[m], cs[m], __fmul2_rn(y.a[m], make_float2(-sn[m].x, -sn[m].y)));
-        ss = __ffma2_rn(x.a[m], x.a[m], ss);
-        ss = __ffma2_rn(x.b[m], x.b[m], ss);
-        y.a[m] = __fmul2_rn(u.a[m], x.a[m]);
-        y.b[m] = __fmul2_rn(u.b[m], x.b[m]);
-        wx = __ffma2_rn(y.a[m], g.a[m], wx);
-        wx = __ffma2_rn(y.b[m], g.b[m], wx);
-        u.a[m] = __fmul2_rn(u.a[m], g.a[m]);
-        u.b[m] = __fmul2_rn(u.b[m], g.b[m]);
+      for (int q = 0; q < 2; ++q) {
+        QnPairs<P> x, y, u;
+        qn_get<T, V, NV, PAIRED>(rx[q], x);
+        qn_get<T, V, NV, PAIRED>(ry[q], y);
+        fetch(j0 + q + 2, rx[q], ry[q]);
+        // u = s Rot(-pos) dy;  t = u x;  sums of x^2 and of g t;  dx = r (g u) - r m x
+        float2 ss = make_float2(0.f, 0.f), wx = ss;
+#pragma unroll
+        for (int m = 0; m < P / 2; ++m) {
+          u.a[m] = __ffma2_rn(y.a[m], cs[m], __fmul2_rn(y.b[m], sn[m]));
+          u.b[m] = __ffma2_rn(y.b[m], cs[m], __fmul2_rn(y.a[m], make_float2(-sn[m].x, -sn[m].y)));
+          ss = __ffma2_rn(x.a[m], x.a[m], ss);
+          ss = __ffma2_rn(x.b[m], x.b[m], ss);
+          y.a[m] = __fmul2_rn(u.a[m], x.a[m]);
+          y.b[m] = __fmul2_rn(u.b[m], x.b[m]);
+          wx = __ffma2_rn(y.a[m], g.a[m], wx);
+          wx = __ffma2_rn(y.b[m], g.b[m], wx);
+          u.a[m] = __fmul2_rn(u.a[m], g.a[m]);
+          u.b[m] = __fmul2_rn(u.b[m], g.b[m]);
+        }
+        const float sum = sh_group_sum<LANES>(ss.x + ss.y), dot = sh_group_sum<LANES>(wx.x + wx.y);
+        float r = rsqrtf(fmaf(sum, inv, a.eps));
+        if (j0 + q >= n) r = 0.f;                        // (no row: what is left of the last one does not count)
+        const float rm = -(dot * inv * r * r) * r;
+        const float2 r2 = make_float2(r, r), rm2 = make_float2(rm, rm);
+#pragma unroll
+        for (int m = 0; m < P / 2; ++m) {
+          dg.a[m] = __ffma2_rn(y.a[m], r2, dg.a[m]);
+          dg.b[m] = __ffma2_rn(y.b[m], r2, dg.b[m]);
+          u.a[m] = __ffma2_rn(x.a[m], rm2, __fmul2_rn(u.a[m], r2));
+          u.b[m] = __ffma2_rn(x.b[m], rm2, __fmul2_rn(u.b[m], r2));
+        }
+        if (j0 + q < n) qn_put<T, V, NV, LANES, PAIRED>(po, col, u);
+        po += s.oh;
       }
-      const float sum = sh_group_sum(ss.x + ss.y, a.lanes), dot = sh_group_sum(wx.x + wx.y, a.lanes);
-      const float r = rsqrtf(fmaf(sum, inv, a.eps)), rm = -(dot * inv * r * r) * r;
-      const float2 r2 = make_float2(r, r), rm2 = make_float2(rm, rm);
-#pragma unroll
-      for (int m = 0; m < P / 2; ++m) {
-        dg.a[m] = __ffma2_rn(y.a[m], r2, dg.a[m]);       // (no row: zeros)
-        dg.b[m] = __ffma2_rn(y.b[m], r2, dg.b[m]);
-        u.a[m] = __ffma2_rn(x.a[m], rm2, __fmul2_rn(u.a[m], r2));
-        u.b[m] = __ffma2_rn(x.b[m], rm2, __fmul2_rn(u.b[m], r2));
-      }
-      if (j < n) qn_put<T, V, NV, PAIRED>(po, col, u);
-#pragma unroll
-      for (int i = 0; i < NV; ++i) po[i] += s.oh;
     }
   }
   if (!s.dgain) return;                                  // (the whole block)
@@ -312,7 +332,7 @@ static __global__ void __launch_bounds__(QN_THREADS, 2) sh_qk_norm_backward_kern
   __syncthreads();
   for (int c = threadIdx.x; c < a.D; c += QN_THREADS) {
     float sum = 0.f;
-    for (int q = 0; q < groups; ++q) sum += s_sum[q * a.D + c];
+    for (int q = 0; q < GROUPS; ++q) sum += s_sum[q * a.D + c];
     a.part[(long long)blockIdx.x * a.D + c] = sum;
   }
 }
@@ -326,9 +346,13 @@ static __global__ void __launch_bounds__(1024) sh_qk_norm_gain_kernel(QnGain a) 
   float* out = a.dgain[side];
   if (!out) return;                                      // (the whole block)
   double sum = 0.0;
-  if (c < a.D)
-#pragma unroll 8
-    for (int i = a.first[side] + threadIdx.y; i < a.first[side + 1]; i += 32) sum += (double)__ldcg(a.part + (long long)i * a.D + c);
+  for (int i = a.first[side] + threadIdx.y; i < a.first[side + 1]; i += 8 * 32) {
+    float v[8];                                          // (loads of a round in flight together)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = c < a.D && i + 32 * k < a.first[side + 1] ? __ldcg(a.part + (long long)(i + 32 * k) * a.D + c) : 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += (double)v[k];
+  }
   s_sum[threadIdx.y][threadIdx.x] = sum;
   __syncthreads();
   if (threadIdx.y == 0 && c < a.D) {

@@ -58,8 +58,9 @@ int vector_width(const sh_qk_norm_args& a, const sh_qk_norm_backward_args* back)
     if (heads > 1) all |= h.head_stride;
   };
   add(a.q, a.q_heads); add(a.q_out, a.q_heads); add(a.k, a.k_heads); add(a.k_out, a.k_heads);
+  for (const float* g : {a.gq, a.gk}) all |= ((uintptr_t)g / 4) & 3;      // (loaded four at a time)
   if (back) { add(back->dq, a.q_heads); add(back->dk, a.k_heads); }
-  int v = 16 / size;
+  int v = back && QN_BACKWARD_V < 16 / size ? QN_BACKWARD_V : 16 / size;
   while (all & (v - 1)) v /= 2;
   return v;
 }
@@ -88,8 +89,8 @@ int qn_check(const sh_qk_norm_args& a, const sh_qk_norm_backward_args* back) {
   return SH_OK;
 }
 
-// The kernel's arguments, for vectors of v values.
-void qn_fill(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, int v, int nv, QnArgs& a) {
+// The kernel's arguments.
+void qn_fill(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, QnArgs& a) {
   const sh_heads none{};
   auto side = [&](QnSide& s, const sh_heads& x, const sh_heads& out, const sh_heads& dy, const float* gain, float* dgain, int heads, float scale) {
     s.x = x.data; s.xb = x.batch_stride; s.xt = x.token_stride; s.xh = x.head_stride;
@@ -104,7 +105,6 @@ void qn_fill(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, int
   a.seq = p.seq; a.D = p.d_head; a.R = p.rotated;
   a.tokens = (long long)p.batch * p.seq;
   a.eps = p.eps;
-  a.lanes = pow2_at_least((p.d_head + v * nv - 1) / (v * nv));
   a.blocks0 = 0; a.part = nullptr;
   // (frequencies by one multiplication each: 64 bits of mantissa, off by a few units of 2^-63 relative at the last)
   if (p.rotated) {
@@ -114,22 +114,39 @@ void qn_fill(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, int
   }
 }
 
-template <typename T, int V, int NV, bool HALVES>
-int qn_launch(const QnArgs& a, bool backward, bool pdl, int blocks, size_t smem, cudaStream_t st) {
-  if (!backward) return launch_k(pdl, sh_qk_norm_kernel<T, V, NV, HALVES>, dim3((unsigned)blocks), dim3(QN_THREADS), 0, st, a);
-  return launch_k(pdl, sh_qk_norm_backward_kernel<T, V, NV, HALVES>, dim3((unsigned)blocks), dim3(QN_THREADS), smem, st, a);
+constexpr int qn_vectors(int v) { return v >= 4 ? 2 : v == 2 ? 4 : 8; }
+// Lanes to a row: 4 to 32 (vectors of two values, where half the rotated width is odd, or less: 16 or 32).
+int qn_lanes(int v, int d_head) {
+  const int n = pow2_at_least((d_head + v * qn_vectors(v) - 1) / (v * qn_vectors(v))), least = v == 8 ? 4 : v == 4 ? 8 : 16;
+  return n > least ? n : least;
 }
 
-constexpr int qn_vectors(int v) { return v >= 4 ? 2 : v == 2 ? 4 : 8; }
+template <typename T, int V, int LANES, bool PAIRED>
+int qn_launch(const QnArgs& a, bool backward, bool pdl, int blocks, cudaStream_t st) {
+  constexpr int NV = qn_vectors(V);
+  if (!backward) return launch_k(pdl, sh_qk_norm_kernel<T, V, NV, LANES, PAIRED>, dim3((unsigned)blocks), dim3(QN_THREADS), 0, st, a);
+  const size_t sums = (size_t)(QN_THREADS / LANES) * a.D * 4;
+  if constexpr (V <= QN_BACKWARD_V) return launch_k(pdl, sh_qk_norm_backward_kernel<T, V, NV, LANES, PAIRED>, dim3((unsigned)blocks), dim3(QN_THREADS), sums, st, a);
+  return SH_ERR_UNSUPPORTED;                               // (vector_width gives the backward kernel no wider ones)
+}
+
+template <typename T, int V, bool PAIRED>
+int qn_lanes_of(const QnArgs& a, int lanes, bool backward, bool pdl, int blocks, cudaStream_t st) {
+  constexpr int LEAST = V == 8 ? 4 : V == 4 ? 8 : 16;
+  if (lanes == LEAST) return qn_launch<T, V, LEAST, PAIRED>(a, backward, pdl, blocks, st);
+  if constexpr (LEAST < 16)
+    if (lanes == 2 * LEAST) return qn_launch<T, V, 2 * LEAST, PAIRED>(a, backward, pdl, blocks, st);
+  return qn_launch<T, V, LEAST < 16 ? 4 * LEAST : 32, PAIRED>(a, backward, pdl, blocks, st);
+}
 
 template <typename T>
-int qn_dispatch(const QnArgs& a, int v, bool halves, bool backward, bool pdl, int blocks, size_t smem, cudaStream_t st) {
+int qn_dispatch(const QnArgs& a, int v, int lanes, bool halves, bool backward, bool pdl, int blocks, cudaStream_t st) {
   if constexpr (sizeof(T) == 2)
-    if (v == 8) return halves ? qn_launch<T, 8, 2, true>(a, backward, pdl, blocks, smem, st) : qn_launch<T, 8, 2, false>(a, backward, pdl, blocks, smem, st);
-  if (v >= 4) return halves ? qn_launch<T, 4, 2, true>(a, backward, pdl, blocks, smem, st) : qn_launch<T, 4, 2, false>(a, backward, pdl, blocks, smem, st);
-  if (v == 2) return halves ? qn_launch<T, 2, 4, true>(a, backward, pdl, blocks, smem, st) : qn_launch<T, 2, 4, false>(a, backward, pdl, blocks, smem, st);
+    if (v == 8) return halves ? qn_lanes_of<T, 8, true>(a, lanes, backward, pdl, blocks, st) : qn_lanes_of<T, 8, false>(a, lanes, backward, pdl, blocks, st);
+  if (v >= 4) return halves ? qn_lanes_of<T, 4, true>(a, lanes, backward, pdl, blocks, st) : qn_lanes_of<T, 4, false>(a, lanes, backward, pdl, blocks, st);
+  if (v == 2) return halves ? qn_lanes_of<T, 2, true>(a, lanes, backward, pdl, blocks, st) : qn_lanes_of<T, 2, false>(a, lanes, backward, pdl, blocks, st);
   // (nothing rotated: d_head may be odd)
-  return a.R ? qn_launch<T, 1, 8, true>(a, backward, pdl, blocks, smem, st) : qn_launch<T, 1, 8, false>(a, backward, pdl, blocks, smem, st);
+  return a.R ? qn_lanes_of<T, 1, true>(a, lanes, backward, pdl, blocks, st) : qn_lanes_of<T, 1, false>(a, lanes, backward, pdl, blocks, st);
 }
 
 int qn_run(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, bool pdl, cudaStream_t st) {
@@ -139,8 +156,8 @@ int qn_run(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, bool 
   const bool halves = p.rotated && p.halves;
   const int v = vector_width(p, back);
   QnArgs a;
-  qn_fill(p, back, v, qn_vectors(v), a);
-  const int groups = QN_THREADS / a.lanes, most = p.q_heads > p.k_heads ? p.q_heads : p.k_heads;
+  qn_fill(p, back, a);
+  const int lanes = qn_lanes(v, p.d_head), groups = QN_THREADS / lanes, most = p.q_heads > p.k_heads ? p.q_heads : p.k_heads;
   // heads to a group: all of them share a token's angles, but not so many that SMs are left without work
   a.per = most < 8 ? (most < 1 ? 1 : most) : 8;
   auto chunks = [&](int i) { return (a.s[i].heads + a.per - 1) / a.per; };
@@ -148,11 +165,10 @@ int qn_run(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, bool 
   a.s[0].chunks = chunks(0); a.s[1].chunks = chunks(1);
   const long long items[2] = {a.tokens * a.s[0].chunks, a.tokens * a.s[1].chunks};
   long long blocks = (items[0] + items[1] + groups - 1) / groups;
-  size_t smem = 0;
   if (backward) {
     long long n[2];
     for (int i = 0; i < 2; ++i) n[i] = (items[i] + groups - 1) / groups;
-    const long long cap = 2ll * sms < QN_MAX_BLOCKS ? 2ll * sms : QN_MAX_BLOCKS;
+    const long long fit = (long long)sms * (p.dtype == SH_F32 ? qn_backward_blocks<float>() : qn_backward_blocks<__half>()), cap = fit < QN_MAX_BLOCKS ? fit : QN_MAX_BLOCKS;
     if (n[0] + n[1] > cap) {                               // shares by the sides' rows
       const long long all = n[0] + n[1];
       const long long b0 = n[0] ? (n[0] * cap + all / 2) / all : 0;
@@ -162,13 +178,12 @@ int qn_run(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, bool 
     a.blocks0 = (int)n[0];
     blocks = n[0] + n[1];
     a.part = (float*)back->workspace;
-    smem = (size_t)groups * p.d_head * 4;
   }
   if (blocks > 0x7fffffffll) { sh_set_error("too many rows: batch * seq * heads / %d must be below 2^31", groups); return SH_ERR_UNSUPPORTED; }
   if (blocks) {
-    int rc = p.dtype == SH_F32 ? qn_dispatch<float>(a, v, halves, backward, pdl, (int)blocks, smem, st)
-           : p.dtype == SH_BF16 ? qn_dispatch<__nv_bfloat16>(a, v, halves, backward, pdl, (int)blocks, smem, st)
-                                : qn_dispatch<__half>(a, v, halves, backward, pdl, (int)blocks, smem, st);
+    int rc = p.dtype == SH_F32 ? qn_dispatch<float>(a, v, lanes, halves, backward, pdl, (int)blocks, st)
+           : p.dtype == SH_BF16 ? qn_dispatch<__nv_bfloat16>(a, v, lanes, halves, backward, pdl, (int)blocks, st)
+                                : qn_dispatch<__half>(a, v, lanes, halves, backward, pdl, (int)blocks, st);
     if (rc) return rc;
   }
   if (backward && (back->dgq || back->dgk)) {

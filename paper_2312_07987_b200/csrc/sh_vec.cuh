@@ -60,8 +60,10 @@ __device__ __forceinline__ void sh_store(T* p, const float (&f)[V]) {
   }
 }
 
-// Sum over groups of `lanes` neighbouring lanes (a power of two), the same in every lane of a group.
-__device__ __forceinline__ float sh_group_sum(float v, int lanes) {
-  for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+// Sum over groups of LANES neighbouring lanes (a power of two), in every lane of a group.
+template <int LANES>
+__device__ __forceinline__ float sh_group_sum(float v) {
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
