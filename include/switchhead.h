@@ -258,7 +258,7 @@ int sh_noalloc_gate_topk(int dtype, int n_tokens, int d_model, int n_heads, int 
                          float* gate, int32_t* offsets, int32_t* lists, void* stream);
 
 /* Backward pass, fp32 configuration of the plain layer (sh_create + sh_configure(SH_F32): two gates,
- * dense Q/K, no cache, no positional term; anything else: SH_ERR_UNSUPPORTED).  The paper gives no
+ * dense Q/K, no cache, no positional term but the rotation of normalised heads; anything else: SH_ERR_UNSUPPORTED).  The paper gives no
  * backward formulas - its training differentiates the forward equations of Sec. 2.2 automatically -
  * so this is the chain rule for those equations with the expert selection held fixed.  Call it after
  * sh_forward(layer, x, ...) on the SAME x (it reads the Q, K, V, Ahat, selections and gates that pass
@@ -377,6 +377,32 @@ typedef struct {
   int32_t dtype, reserved;
 } sh_dropout_args;
 int sh_dropout(const sh_dropout_args* args, void* stream);
+
+/* The same as parts of the fp32 layer's own passes.  Host calls, no launch; they take effect with the next sh_forward, and end with
+ * sh_configure / sh_set_workspace.  All pointers are device pointers of the caller, read or written by the passes: they stay
+ * valid as long as the setting does.  A scratch holds sh_training_scratch_bytes(layer, which) bytes, aligned to 256, of one
+ * layer; sh_backward reads what the forward pass left there (without it - where it may be NULL - sh_backward has no pass to
+ * differentiate).  sh_backward differentiates the pass that was made, with its settings.  SH_ERR_UNSUPPORTED for bf16
+ * storage and the dense comparator. */
+enum { SH_SCRATCH_QK_NORM = 0, SH_SCRATCH_BALANCE = 1, SH_SCRATCH_DROPOUT = 2 };
+size_t sh_training_scratch_bytes(const sh_layer* layer, int which);     /* 0: not configured, or not such a layer */
+
+/* Q and K are normalised per head (gains gq, gk [d_head] or NULL) between their projection and the attention, as sh_qk_norm
+ * does it; with sh_set_rope the rotation follows in the same pass, and sh_backward then serves the layer with rotary positions.
+ * sh_backward writes the gains' gradients to dgq, dgk [d_head] (NULL: not wanted).  scratch may be NULL (forward passes only).
+ * eps = 0 switches the norms off.  Not with query / key experts or the relative-position term. */
+int sh_set_qk_norm(sh_layer* layer, const float* gq, const float* gk, float eps, float* dgq, float* dgk, void* scratch, size_t scratch_bytes);
+
+/* sh_forward also gives the balance loss of its gates (of all tokens the layer sees, or those of mask [N]; one gate per head and
+ * side): loss [1], counts and prob [sides, H, E] as sh_balance_loss.  sh_backward adds *gloss (NULL: 1) times its
+ * gradient to those of the gates, so to dx, dWs and dWd.  loss = scratch = NULL switches it off. */
+int sh_set_balance(sh_layer* layer, int kind, float coef, const void* mask, float* loss, int32_t* counts, float* prob, const float* gloss,
+                   void* scratch, size_t scratch_bytes);
+
+/* out of sh_forward goes through dropout (rows: those of out, columns: d_model, as sh_dropout); sh_backward takes dout back
+ * through the same mask, so the two values of rng must not change between them.  scratch may be NULL (forward passes only).
+ * rng = NULL switches it off. */
+int sh_set_dropout(sh_layer* layer, double p, const void* rng, void* scratch, size_t scratch_bytes);
 
 /* Device pointer and size of an intermediate buffer inside the workspace (contents are
  * those of the last sh_forward / sh_gate_topk once the stream has drained).  Element type:

@@ -29,7 +29,7 @@ EXPORTS = ["sh_create", "sh_create_shared", "sh_create_moe_qk", "sh_create_dense
            "sh_noalloc_gate_topk", "sh_debug_buffer", "sh_last_status", "sh_status_block", "sh_clear_status", "sh_check_guards",
            "sh_selftest", "sh_set_output_f16", "sh_is_debug_build", "sh_launch_count", "sh_last_error", "sh_destroy",
            "sh_qk_norm", "sh_qk_norm_backward", "sh_qk_norm_workspace_bytes", "sh_balance_loss", "sh_balance_backward",
-           "sh_balance_workspace_bytes", "sh_dropout"]
+           "sh_balance_workspace_bytes", "sh_dropout", "sh_training_scratch_bytes", "sh_set_qk_norm", "sh_set_balance", "sh_set_dropout"]
 STAMP_KERNELS = ["gate", "sort", "qk_a", "qk_b", "v", "attn", "o"]
 
 
@@ -102,6 +102,14 @@ def _load() -> ctypes.CDLL:
     lib.sh_qk_norm_workspace_bytes.argtypes = [i32]
     lib.sh_balance_workspace_bytes.restype = sz
     lib.sh_balance_workspace_bytes.argtypes = [i32] * 3
+    lib.sh_training_scratch_bytes.restype = sz
+    lib.sh_training_scratch_bytes.argtypes = [vp, i32]
+    lib.sh_set_qk_norm.restype = i32
+    lib.sh_set_qk_norm.argtypes = [vp, vp, vp, ctypes.c_float, vp, vp, vp, sz]
+    lib.sh_set_balance.restype = i32
+    lib.sh_set_balance.argtypes = [vp, i32, ctypes.c_float] + [vp] * 6 + [sz]
+    lib.sh_set_dropout.restype = i32
+    lib.sh_set_dropout.argtypes = [vp, ctypes.c_double, vp, vp, sz]
     lib.sh_destroy.restype = None
     lib.sh_destroy.argtypes = [vp]
     return lib
@@ -191,6 +199,46 @@ class Layer:
     def sh_set_rope(self, base: float) -> None:
         _check(lib.sh_set_rope(self.handle, float(base), _stream()))
 
+    def _scratch(self, which: int):
+        """A scratch of a training setting, and its bytes."""
+        n = lib.sh_training_scratch_bytes(self.handle, which)
+        return torch.empty(n, dtype=torch.uint8, device=self.workspace.device) if n else None, n
+
+    def sh_set_qk_norm(self, gq=None, gk=None, eps: float = 1e-6, train: bool = True) -> None:
+        """Q and K normalised per head between projection and attention (fp32 layers), gains gq, gk [d_head] fp32 device tensors or None;
+        eps = 0 switches it off.  train: sh_backward returns dgq and dgk of the gains that are given."""
+        D = self.dims[2]
+        for g in (gq, gk):
+            assert g is None or (g.is_cuda and g.is_contiguous() and g.dtype == torch.float32 and tuple(g.shape) == (D,))
+        grads = [torch.empty_like(g) if g is not None and train else None for g in (gq, gk)]
+        scratch, n = self._scratch(0) if train and eps else (None, 0)
+        _check(lib.sh_set_qk_norm(self.handle, _ptr(gq), _ptr(gk), eps, _ptr(grads[0]), _ptr(grads[1]), _ptr(scratch), n))
+        self._qk_norm = (gq, gk, *grads, scratch)          # (the passes read and write them)
+
+    def sh_set_balance(self, kind: Optional[str], coef: float = 0.01, mask: Optional[torch.Tensor] = None, gloss: Optional[torch.Tensor] = None) -> Optional[dict]:
+        """sh_forward also gives the balance loss of its gates (fp32 layers): returns the tensors it writes, {loss, counts, prob}; sh_backward
+        adds gloss times its gradient to the gates'.  kind: "counts", "entropy", or None to switch it off.  mask [batch * seq] bool: tokens that count."""
+        if kind is None:
+            _check(lib.sh_set_balance(self.handle, 0, 0.0, *([None] * 6), 0))
+            self._balance = None
+            return None
+        dev, (_, H, _, E, _) = self.workspace.device, self.dims
+        assert mask is None or (mask.is_cuda and mask.is_contiguous() and mask.dtype in (torch.bool, torch.uint8) and mask.numel() == self.batch * self.seq)
+        assert gloss is None or (gloss.is_cuda and gloss.dtype == torch.float32 and gloss.numel() == 1)
+        sides = 1 if self.shared_selection else 2
+        out = dict(loss=torch.empty((), device=dev), counts=torch.empty((sides, H, E), dtype=torch.int32, device=dev), prob=torch.empty((sides, H, E), device=dev))
+        scratch, n = self._scratch(1)
+        _check(lib.sh_set_balance(self.handle, SH_BALANCE[kind], coef, _ptr(mask), _ptr(out["loss"]), _ptr(out["counts"]), _ptr(out["prob"]), _ptr(gloss), _ptr(scratch), n))
+        self._balance = (mask, gloss, out, scratch)
+        return out
+
+    def sh_set_dropout(self, p: float, rng: Optional[torch.Tensor], train: bool = True) -> None:
+        """Dropout of sh_forward's output (fp32 layers); rng: a device tensor of two int64, seed and offset, which the passes read (None: off)."""
+        assert rng is None or (rng.is_cuda and rng.dtype == torch.int64 and rng.is_contiguous() and rng.numel() == 2)
+        scratch, n = self._scratch(2) if train and rng is not None else (None, 0)
+        _check(lib.sh_set_dropout(self.handle, p, _ptr(rng), _ptr(scratch), n))
+        self._dropout = (rng, scratch)
+
     def sh_set_output_f16(self, enable: bool) -> None:
         """sh_forward writes fp16 instead of fp32 from now on (bf16 storage configuration only)."""
         _check(lib.sh_set_output_f16(self.handle, 1 if enable else 0))
@@ -233,13 +281,17 @@ class Layer:
         _check(lib.sh_selftest(self.handle, which, arg, _stream()))
 
     def sh_backward(self, x: torch.Tensor, dout: torch.Tensor) -> dict:
-        """Gradients of sum(out * dout) with respect to x and every weight (fp32 configuration; call sh_forward(x) first)."""
+        """Gradients of sum(out * dout) with respect to x and every weight (fp32 configuration; call sh_forward(x) first), and of the gains of
+        sh_set_qk_norm (dgq, dgk)."""
         d_model, H, D, E, k = self.dims
         dev = x.device
         z = lambda *shape: torch.empty(shape, dtype=torch.float32, device=dev)
         g = dict(dx=z(self.batch, self.seq, d_model), dWq=z(H, d_model, D), dWk=z(H, d_model, D), dWv=z(H, E, d_model, D),
                  dWo=z(H, E, D, d_model), dWs=z(H, d_model, E), dWd=z(H, d_model, E))
         _check(lib.sh_backward(self.handle, _ptr(x), _ptr(dout), *[_ptr(g[n]) for n in ("dx", "dWq", "dWk", "dWv", "dWo", "dWs", "dWd")], _stream()))
+        for name, grad in zip(("dgq", "dgk"), getattr(self, "_qk_norm", (None,) * 4)[2:4]):
+            if grad is not None:
+                g[name] = grad.clone()
         return g
 
     def sh_gate_topk(self, x: torch.Tensor):

@@ -201,7 +201,7 @@ static int configure_common(sh_layer* L, int dtype, int batch, int seq, int cach
   //  passes have been seen 1e-2 of the output RMS apart; with the first rows, which reach the output
   //  unaveraged, summed in fp32 they stay within 4e-3)
   L->d.early_rows = (dtype == SH_BF16 && (T >= SH_EARLY_MIN_SEQ || d0.k >= 3)) ? SH_EARLY_ROWS : 0;
-  L->ws = nullptr; L->ws_bytes = 0; L->rope = false; L->xl_positions = false;
+  L->ws = nullptr; L->ws_bytes = 0; L->rope = false; L->xl_positions = false; L->train = ShTraining();
   L->fwd_x = nullptr;
   L->d.status = nullptr;
   L->weights_set = false;
@@ -229,7 +229,7 @@ extern "C" int sh_set_workspace(sh_layer* L, void* workspace, size_t bytes) {
   if (!workspace) { sh_set_error("workspace is NULL"); return SH_ERR_WORKSPACE; }
   if ((uintptr_t)workspace % 256 != 0) { sh_set_error("workspace must be 256-byte aligned"); return SH_ERR_WORKSPACE; }
   if (bytes < L->o.total) { sh_set_error("workspace too small: %zu bytes given, %zu needed", bytes, L->o.total); return SH_ERR_WORKSPACE; }
-  L->ws = (char*)workspace; L->ws_bytes = bytes; L->weights_set = false; L->rope = false; L->xl_positions = false;
+  L->ws = (char*)workspace; L->ws_bytes = bytes; L->weights_set = false; L->rope = false; L->xl_positions = false; L->train = ShTraining();
   L->fwd_x = nullptr;
   L->d.status = (int*)(L->ws + L->o.status);
   sh_tc_release(L);
@@ -589,6 +589,7 @@ extern "C" int sh_set_xl_positions(sh_layer* L, const float* Wr, const float* u,
     return SH_ERR_UNSUPPORTED;
   }
   if (L->rope) { sh_set_error("rotary embeddings are switched on: one positional encoding at a time"); return SH_ERR_UNSUPPORTED; }
+  if (L->train.norm.on) { sh_set_error("norms of queries and keys do not go with the relative-position term"); return SH_ERR_UNSUPPORTED; }
   const ShDims& d = L->d;
   if (d.M % 2) { sh_set_error("the sinusoidal embedding needs an even d_model"); return SH_ERR_UNSUPPORTED; }
   cudaStream_t st = (cudaStream_t)stream;
@@ -619,7 +620,7 @@ extern "C" int sh_set_rope(sh_layer* L, double base, void* stream) {
   if (!L) { sh_set_error("layer is NULL"); return SH_ERR_INVALID_ARG; }
   if (L->dtype < 0 || !L->ws) { sh_set_error("sh_set_rope needs a configured layer with its workspace"); return SH_ERR_NOT_CONFIGURED; }
   if (!(base >= 0.0) || base != base) { sh_set_error("rotary base must be positive (0 switches it off), got %g", base); return SH_ERR_INVALID_ARG; }
-  if (base == 0.0) { L->rope = false; return SH_OK; }
+  if (base == 0.0) { L->rope = false; L->train.norm.base = 0.0; return SH_OK; }
   if (L->xl_positions) { sh_set_error("relative positions are switched on: one positional encoding at a time"); return SH_ERR_UNSUPPORTED; }
   if (L->d.Tc > 0) { sh_set_error("rotary embeddings are for the cache-less layer (the paper's RoPE models have no cache)"); return SH_ERR_UNSUPPORTED; }
   if (L->d.Dt % 2) { sh_set_error("rotary embedding needs an even d_head (got %d)", L->d.Dt); return SH_ERR_UNSUPPORTED; }
@@ -628,6 +629,74 @@ extern "C" int sh_set_rope(sh_layer* L, double base, void* stream) {
   sh_rope_table_kernel<<<(n + 255) / 256, 256, 0, (cudaStream_t)stream>>>((float2*)(L->ws + L->o.rope), L->d.T, L->d.D, L->d.Dt, base);
   SH_CUDA_CHECK(cudaGetLastError());
   L->rope = true;
+  L->rope_base = base;
+  L->train.norm.base = base;                               // (with norms of queries and keys the rotation is theirs)
+  return SH_OK;
+}
+
+// Whether a layer may have what a training step adds; `what` names it.
+static int training_ok(sh_layer* L, const char* what) {
+  g_err[0] = 0;
+  if (!L) { sh_set_error("layer is NULL"); return SH_ERR_INVALID_ARG; }
+  if (L->dtype < 0 || !L->ws) { sh_set_error("%s needs a configured layer with its workspace", what); return SH_ERR_NOT_CONFIGURED; }
+  if (L->dtype != SH_F32 || L->dense) { sh_set_error("%s: the fp32 configuration of the SwitchHead layer only", what); return SH_ERR_UNSUPPORTED; }
+  return SH_OK;
+}
+static int scratch_ok(const char* what, const void* p, size_t bytes, size_t need, bool optional) {
+  if (!p && optional) return SH_OK;
+  if (!p || (uintptr_t)p % 256 != 0) { sh_set_error("%s: scratch must be a device pointer aligned to 256 bytes", what); return SH_ERR_WORKSPACE; }
+  if (bytes < need) { sh_set_error("%s: scratch too small: %zu bytes given, %zu needed", what, bytes, need); return SH_ERR_WORKSPACE; }
+  return SH_OK;
+}
+
+extern "C" size_t sh_training_scratch_bytes(const sh_layer* L, int which) {
+  if (!L || L->dtype != SH_F32 || L->dense) return 0;
+  return which == SH_SCRATCH_QK_NORM ? sh_f32_norm_scratch(L) : which == SH_SCRATCH_BALANCE ? sh_f32_balance_scratch(L)
+       : which == SH_SCRATCH_DROPOUT ? sh_f32_dropout_scratch(L) : 0;
+}
+
+extern "C" int sh_set_qk_norm(sh_layer* L, const float* gq, const float* gk, float eps, float* dgq, float* dgk, void* scratch, size_t bytes) {
+  const char* what = "sh_set_qk_norm";
+  if (int rc = training_ok(L, what)) return rc;
+  if (!(eps >= 0.f) || eps > 3.0e38f) { sh_set_error("eps must be positive and finite (0 switches the norms off), got %g", (double)eps); return SH_ERR_INVALID_ARG; }
+  if (eps == 0.f) { L->train.norm = ShQkNorm(); L->train.norm.base = L->rope ? L->rope_base : 0.0; return SH_OK; }
+  if (L->moe_q || L->moe_k) { sh_set_error("norms of queries and keys follow the dense Q/K projection: not with query / key experts"); return SH_ERR_UNSUPPORTED; }
+  if (L->xl_positions) { sh_set_error("norms of queries and keys do not go with the relative-position term"); return SH_ERR_UNSUPPORTED; }
+  if ((dgq || dgk) && !scratch) { sh_set_error("gradients of the gains need the scratch"); return SH_ERR_INVALID_ARG; }
+  if (int rc = scratch_ok(what, scratch, bytes, sh_f32_norm_scratch(L), true)) return rc;
+  ShQkNorm n;
+  n.on = true; n.eps = eps; n.base = L->rope ? L->rope_base : 0.0;
+  n.gq = gq; n.gk = gk; n.dgq = dgq; n.dgk = dgk; n.scratch = (char*)scratch;
+  L->train.norm = n;
+  return SH_OK;
+}
+
+extern "C" int sh_set_balance(sh_layer* L, int kind, float coef, const void* mask, float* loss, int32_t* counts, float* prob, const float* gloss, void* scratch,
+                              size_t bytes) {
+  const char* what = "sh_set_balance";
+  if (int rc = training_ok(L, what)) return rc;
+  if (!scratch && !loss) { L->train.balance = ShBalance(); return SH_OK; }
+  if (kind != SH_BALANCE_COUNTS && kind != SH_BALANCE_ENTROPY) { sh_set_error("unknown kind of balance loss: %d", kind); return SH_ERR_INVALID_ARG; }
+  if (!(coef - coef == 0.f)) { sh_set_error("coef must be finite (got %g)", (double)coef); return SH_ERR_INVALID_ARG; }
+  if (!loss || !counts || !prob) { sh_set_error("loss, counts and prob must not be NULL"); return SH_ERR_INVALID_ARG; }
+  if ((long long)L->d.sides * L->d.H > 65535) { sh_set_error("sides * n_heads must be at most 65535"); return SH_ERR_UNSUPPORTED; }
+  if (int rc = scratch_ok(what, scratch, bytes, sh_f32_balance_scratch(L), false)) return rc;
+  ShBalance b;
+  b.on = true; b.kind = kind; b.coef = coef; b.mask = mask; b.loss = loss; b.counts = counts; b.prob = prob; b.gloss = gloss; b.scratch = (char*)scratch;
+  L->train.balance = b;
+  return SH_OK;
+}
+
+extern "C" int sh_set_dropout(sh_layer* L, double p, const void* rng, void* scratch, size_t bytes) {
+  const char* what = "sh_set_dropout";
+  if (int rc = training_ok(L, what)) return rc;
+  if (!rng) { L->train.dropout = ShDropout(); return SH_OK; }
+  if (!(p >= 0.0 && p <= 1.0)) { sh_set_error("p must be in 0..1 (got %g)", p); return SH_ERR_INVALID_ARG; }
+  if ((uintptr_t)rng % 8) { sh_set_error("rng must be aligned to 8 bytes"); return SH_ERR_INVALID_ARG; }
+  if (int rc = scratch_ok(what, scratch, bytes, sh_f32_dropout_scratch(L), true)) return rc;
+  ShDropout o;
+  o.on = true; o.p = p; o.rng = rng; o.scratch = (char*)scratch;
+  L->train.dropout = o;
   return SH_OK;
 }
 
@@ -642,8 +711,12 @@ extern "C" int sh_forward(sh_layer* L, const void* x, void* out, void* stream) {
   L->fwd_x = nullptr; L->fwd_causal = L->d.causal;
   if (L->dtype == SH_BF16) return sh_tc_forward(L, x, out, st);
   rc = L->dense ? forward_simt<float, float>(L, SH_STAGE_ALL, x, out, st) : sh_f32_forward(L, x, out, st);
-  // (a pass with a positional term leaves rotated Q and K, or no row maxima: not what sh_backward differentiates)
-  if (rc == SH_OK && !L->rope && !L->xl_positions) L->fwd_x = x;
+  // (a pass with a positional term leaves rotated Q and K, or no row maxima: not what sh_backward differentiates - unless the
+  //  rotation is that of the norms, which kept what they were given)
+  const ShTraining& tr = L->train;
+  const bool heads_ok = tr.norm.on ? tr.norm.scratch != nullptr : !L->rope;
+  if (rc == SH_OK && heads_ok && !L->xl_positions && (!tr.dropout.on || tr.dropout.scratch)) L->fwd_x = x;
+  L->fwd_train = tr;
   return rc;
 }
 
@@ -652,8 +725,9 @@ extern "C" int sh_backward(sh_layer* L, const void* x, const float* dout, float*
   g_err[0] = 0;
   int rc = check_ready(L);
   if (rc != SH_OK) return rc;
-  if (L->dtype != SH_F32 || L->dense || L->d.sides != 2 || L->d.Tc > 0 || L->rope || L->xl_positions || L->moe_q || L->moe_k) {
-    sh_set_error("sh_backward serves the fp32 configuration of the plain layer (two gates, dense Q/K, no cache, no positional term)");
+  if (L->dtype != SH_F32 || L->dense || L->d.sides != 2 || L->d.Tc > 0 || (L->rope && !L->fwd_train.norm.on) || L->xl_positions || L->moe_q || L->moe_k) {
+    sh_set_error("sh_backward serves the fp32 configuration of the plain layer (two gates, dense Q/K, no cache, no positional term but "
+                 "the rotation of normalised heads)");
     return SH_ERR_UNSUPPORTED;
   }
   if (!x || !dout || !dx || !dWq || !dWk || !dWv || !dWo || !dWs || !dWd) { sh_set_error("sh_backward: NULL argument"); return SH_ERR_INVALID_ARG; }

@@ -146,8 +146,9 @@ void use_side(XGemmArgs& g, sh_layer* L, int side) {
   g.tiles = (const ShTile*)(ws + L->o.tiles) + (size_t)side * d.max_tiles;
 }
 
-// Gates, selection and sort; beside them `zero` (n values), which a later kernel adds into, is cleared.
-int launch_gate_sort(sh_layer* L, const void* x, float* zero, long n, cudaStream_t st) {
+// Gates, selection and sort; beside them `zero` (n values), which a later kernel adds into, is cleared.  logits: where the gate
+// logits go as well, or nullptr.
+int launch_gate_sort(sh_layer* L, const void* x, float* zero, long n, cudaStream_t st, float* logits = nullptr) {
   const ShDims& d = L->d;
   char* ws = L->ws;
   // eight tokens a block while sixteen would leave SMs with less than two blocks (or their logits do not fit)
@@ -165,7 +166,7 @@ int launch_gate_sort(sh_layer* L, const void* x, float* zero, long n, cudaStream
     SH_CUDA_CHECK(cudaMemsetAsync(ws + L->o.tiles, 0, (size_t)2 * d.max_tiles * sizeof(ShTile), st));
   }
   if (int rc = launch_k(chained(L), kern, dim3((unsigned)((d.N + tok - 1) / tok)), dim3(512), smem, st, (const float*)x, (const float*)(ws + L->o.wgate32),
-                        (const float*)(ws + L->o.gbias), (int*)(ws + L->o.idx), (float*)(ws + L->o.gate), blockcnt, (float4*)zero, n / 4, d, (int)((uintptr_t)x % 16 == 0)))
+                        (const float*)(ws + L->o.gbias), (int*)(ws + L->o.idx), (float*)(ws + L->o.gate), blockcnt, logits, (float4*)zero, n / 4, d, (int)((uintptr_t)x % 16 == 0)))
     return rc;
   L->launches += 2;
   if (blockcnt) {
@@ -272,6 +273,48 @@ int launch_attn(sh_layer* L, float* zero, long n, cudaStream_t st) {
   }
 }
 
+// ---- what a training step adds (sh_set_qk_norm, sh_set_balance, sh_set_dropout) ----
+
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+size_t raw_heads(const ShDims& d) { return (size_t)d.N * d.H * d.D; }        // values of all queries, or of all keys
+
+// Queries and keys: as projected (the scratch, or where they stay) -> normalised, rotated, the queries scaled for the attention.
+sh_qk_norm_args norm_args(sh_layer* L, const ShQkNorm& n) {
+  const ShDims& d = L->d;
+  char* ws = L->ws;
+  const int64_t row = d.D, head = (int64_t)d.T * d.D, seq = (int64_t)d.H * d.T * d.D;
+  auto at = [&](void* p) { return sh_heads{p, seq, row, head}; };
+  sh_qk_norm_args a{};
+  a.q_out = at(ws + L->o.q); a.k_out = at(ws + L->o.k);
+  a.q = n.scratch ? at(n.scratch) : a.q_out;
+  a.k = n.scratch ? at((float*)n.scratch + raw_heads(d)) : a.k_out;
+  a.gq = n.gq; a.gk = n.gk;
+  a.base = n.base; a.rotated = n.base > 0.0 ? d.Dt : 0;
+  a.dtype = SH_F32; a.batch = d.B; a.seq = d.T; a.q_heads = a.k_heads = d.H; a.d_head = d.Dt;
+  a.eps = n.eps; a.q_scale = 1.4426950408889634f / sqrtf((float)d.Dt);
+  return a;
+}
+
+sh_balance_args balance_args(sh_layer* L, const ShBalance& b) {
+  const ShDims& d = L->d;
+  sh_balance_args a{};
+  a.n_tokens = d.N; a.token_stride = d.G; a.logits = b.scratch;
+  a.idx = (const int*)(L->ws + L->o.idx); a.mask = b.mask; a.gloss = b.gloss;
+  a.loss = b.loss; a.prob = b.prob; a.counts = b.counts;
+  const size_t logits = up256((size_t)d.N * d.G * 4), slope = up256((size_t)d.G * 4);
+  a.slope = (float*)(b.scratch + logits);
+  a.workspace = b.scratch + logits + slope; a.workspace_bytes = sh_balance_workspace_bytes(d.sides, d.H, d.E);
+  a.dtype = SH_F32; a.kind = b.kind; a.sides = d.sides; a.n_heads = d.H; a.n_experts = d.E; a.k = d.k; a.coef = b.coef;
+  return a;
+}
+
+sh_dropout_args dropout_args(sh_layer* L, const ShDropout& o, const void* x, void* y) {
+  const ShDims& d = L->d;
+  sh_dropout_args a{};
+  a.x = x; a.y = y; a.rng = o.rng; a.rows = sh_out_rows(d); a.cols = a.x_stride = a.y_stride = d.M; a.p = o.p; a.dtype = SH_F32;
+  return a;
+}
+
 struct BwBuffers { float *dq, *dk, *dv, *dahat, *dz, *dsum; size_t cleared; };
 BwBuffers bw_buffers(sh_layer* L) {
   const ShDims& d = L->d;
@@ -338,6 +381,13 @@ int sh_f32_prepare(sh_layer* L) {
   return SH_OK;
 }
 
+size_t sh_f32_norm_scratch(const sh_layer* L) { return up256(2 * raw_heads(L->d) * 4) + sh_qk_norm_workspace_bytes(L->d.Dt); }
+size_t sh_f32_balance_scratch(const sh_layer* L) {
+  const ShDims& d = L->d;
+  return up256((size_t)d.N * d.G * 4) + up256((size_t)d.G * 4) + sh_balance_workspace_bytes(d.sides, d.H, d.E);
+}
+size_t sh_f32_dropout_scratch(const sh_layer* L) { return (size_t)sh_out_rows(L->d) * L->d.M * 4; }
+
 void sh_f32_release(sh_layer* L) {
   if (L && L->f32) { delete (F32State*)L->f32; L->f32 = nullptr; }
 }
@@ -368,9 +418,19 @@ int sh_f32_forward(sh_layer* L, const void* x, void* out, cudaStream_t st) {
   // Dense queries and keys (a layer with query / key experts has none of its own) and the value experts
   // need nothing of one another: one launch, in a stage-timed pass two.
   const int first = L->moe_q ? d.H : 0, groups = (L->moe_q ? 0 : d.H) + (L->moe_k ? 0 : d.H);
-  const XPart qk = part_qk(L, x, first, groups), pv = part_v(L, x, 0, S->wv, v, 0.f);
+  const ShTraining& tr = L->train;
+  XPart qk = part_qk(L, x, first, groups);
+  const XPart pv = part_v(L, x, 0, S->wv, v, 0.f);
+  if (tr.norm.on) {                                         // (the norm rotates and scales behind it)
+    qk.g.rope = nullptr; qk.g.qscale = 1.f;
+    if (tr.norm.scratch) { qk.g.q = (float*)tr.norm.scratch; qk.g.k = qk.g.q + raw_heads(d); }
+  }
   sh_mark(L, 0, st);
-  if ((rc = launch_gate_sort(L, x, v, nhd, st))) return rc;
+  if ((rc = launch_gate_sort(L, x, v, nhd, st, tr.balance.on ? (float*)tr.balance.scratch : nullptr))) return rc;
+  if (tr.balance.on) {
+    if ((rc = sh_run_balance_loss(balance_args(L, tr.balance), chained(L), st))) return rc;
+    L->launches += 2;
+  }
   sh_mark(L, 1, st);
   if (L->ev && (rc = launch_x<X_QK>(L, st, qk))) return rc;
   if (L->moe_k) {
@@ -383,6 +443,10 @@ int sh_f32_forward(sh_layer* L, const void* x, void* out, cudaStream_t st) {
   }
   sh_mark(L, 2, st);
   if ((rc = L->ev ? launch_x<X_V>(L, st, pv) : launch_x<X_QK, X_V>(L, st, qk, pv))) return rc;
+  if (tr.norm.on) {
+    if ((rc = sh_run_qk_norm(norm_args(L, tr.norm), chained(L), st))) return rc;
+    L->launches += 1;
+  }
   sh_mark(L, 3, st);
   // (the relative-position term of Transformer-XL is in the one-warp-per-query kernel only; `out` is cleared
   //  behind the last read of x either way: the two may be the same buffer)
@@ -393,6 +457,10 @@ int sh_f32_forward(sh_layer* L, const void* x, void* out, cudaStream_t st) {
   use_side(g, L, 1);
   g.y = (float*)out;
   if ((rc = launch_d<X_O>(L, st, g))) return rc;
+  if (tr.dropout.on) {
+    if ((rc = sh_run_dropout(dropout_args(L, tr.dropout, out, out), chained(L), st))) return rc;
+    L->launches += 1;
+  }
   sh_mark(L, 5, st);
   SH_CUDA_CHECK(cudaGetLastError());
   return SH_OK;
@@ -406,6 +474,12 @@ int sh_f32_backward(sh_layer* L, const void* x, const float* dout, float* dx, fl
   const int ht = head_tiles(d), mt = (d.M + 127) / 128;
   int rc;
   L->launches = 0;
+  const ShTraining& tr = L->fwd_train;
+  int more = 0;
+  if (tr.dropout.on) {                                      // behind the mask of the forward pass
+    if ((rc = sh_run_dropout(dropout_args(L, tr.dropout, dout, tr.dropout.scratch), false, st))) return rc;
+    dout = (const float*)tr.dropout.scratch; ++more;
+  }
   XGemmArgs src = base_args(L, x);                         // source side; dst: destination side
   src.dy = dout; src.dq = w.dq; src.dk = w.dk; src.dv = w.dv; src.dz = w.dz; src.dsum = w.dsum; src.dahat = w.dahat; src.dx = dx;
   src.dWq = dWq; src.dWk = dWk; src.dWv = dWv; src.dWo = dWo; src.dWs = dWs; src.dWd = dWd;
@@ -439,6 +513,12 @@ int sh_f32_backward(sh_layer* L, const void* x, const float* dout, float* dx, fl
   if (gq.ksplit > 1) { clear(dWq, hmd); clear(dWk, hmd); clear(dWs, hme); clear(dWd, hme); }
   if (gv.ksplit > 1) { clear(dWv, hmd * d.E); clear(dWo, hmd * d.E); }
   if ((rc = launch_k(chained(L), sh_f32_clear_kernel, dim3(4u * (unsigned)sm_count(L)), dim3(256), 0, st, c))) return rc;
+  if (tr.balance.on) {                                      // the gates' gradients begin with the balance loss's
+    sh_balance_args a = balance_args(L, tr.balance);
+    a.dlogits = w.dz; a.dtoken_stride = sh_f32_ldz(d);
+    if ((rc = sh_run_balance_backward(a, true, chained(L), st))) return rc;
+    ++more;
+  }
   XGemmArgs g;
   // output experts: dAhat and the destination gates' gradients
   g = dst;
@@ -450,6 +530,18 @@ int sh_f32_backward(sh_layer* L, const void* x, const float* dout, float* dx, fl
   rc = d.D == 32 ? launch_attn_bw_t<32>(L, w, st) : d.D == 64 ? launch_attn_bw_t<64>(L, w, st)
      : d.D == 128 ? launch_attn_bw_t<128>(L, w, st) : launch_attn_bw_t<256>(L, w, st);
   if (rc) return rc;
+  if (tr.norm.on) {                                         // dq, dk: of the finished queries and keys -> of the projected ones, in place
+    sh_qk_norm_backward_args a{};
+    a.norm = norm_args(L, tr.norm);
+    const int64_t row = (int64_t)d.H * d.D;
+    a.dq = a.norm.q_out = sh_heads{w.dq, d.T * row, row, d.D};
+    a.dk = a.norm.k_out = sh_heads{w.dk, d.T * row, row, d.D};
+    a.norm.q_scale = 1.f;                                   // (the attention's gradient is that of the query before its scale)
+    a.dgq = tr.norm.dgq; a.dgk = tr.norm.dgk;
+    a.workspace = tr.norm.scratch + up256(2 * raw_heads(d) * 4); a.workspace_bytes = sh_qk_norm_workspace_bytes(d.Dt);
+    if ((rc = sh_run_qk_norm_backward(a, chained(L), st))) return rc;
+    more += a.dgq || a.dgk ? 2 : 1;
+  }
   // value experts: their part of dx, and the source gates' gradients
   if ((rc = launch_d<X_DR>(L, st, src))) return rc;
   // queries, keys and gates: the rest of dx
@@ -462,6 +554,6 @@ int sh_f32_backward(sh_layer* L, const void* x, const float* dout, float* dx, fl
   if ((rc = set_smem(sh_f32_wgrad_kernel, XWgradSmem::TOTAL))) return rc;
   if ((rc = launch_k(chained(L), sh_f32_wgrad_kernel, dim3((unsigned)(pq.n + pv.n + po.n)), dim3(XW_THREADS), XWgradSmem::TOTAL, st, pq, pv, po))) return rc;
   SH_CUDA_CHECK(cudaGetLastError());
-  L->launches += 3;
+  L->launches += 3 + more;
   return SH_OK;
 }

@@ -53,7 +53,7 @@ __device__ __forceinline__ void sh_select(float* z, const float* __restrict__ gb
 template <int TOK, int CH>
 static __global__ void __launch_bounds__(512, 1)
 sh_f32_gate_kernel(const float* __restrict__ x, const float* __restrict__ wgate, const float* __restrict__ gbias, int* __restrict__ idx,
-                   float* __restrict__ gate, int* __restrict__ blockcnt, float4* __restrict__ zero, long nzero, ShDims d, int vec) {
+                   float* __restrict__ gate, int* __restrict__ blockcnt, float* __restrict__ logits, float4* __restrict__ zero, long nzero, ShDims d, int vec) {
   extern __shared__ __align__(16) float gsm[];             // [TOK][CH] of x, then [TOK][G] logits
   float* s_z = gsm + TOK * CH;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -125,6 +125,10 @@ sh_f32_gate_kernel(const float* __restrict__ x, const float* __restrict__ wgate,
   for (int i = tid; i < TOK * groups; i += 512) {
     const int r = i / groups, grp = i % groups;
     if (t0 + r < d.N) sh_select(s_z + r * d.G + grp * d.E, gbias, idx, gate, blockcnt, d, t0 + r, grp);
+  }
+  if (logits) {                                             // [N, G], for the balance loss
+    __syncthreads();
+    for (int i = tid; i < min(TOK, d.N - t0) * d.G; i += 512) logits[(size_t)t0 * d.G + i] = s_z[i];
   }
 }
 

@@ -126,8 +126,37 @@ enum {
 #define SH_GUARD_BYTE 0xC5u
 #define SH_MAX_GUARDS 40
 
+// What a training step adds to the fp32 layer's passes; the pointers are the caller's.
+struct ShQkNorm {                      // sh_set_qk_norm
+  bool on = false;
+  float eps = 0.f;
+  double base = 0.0;                   // rotation in the same pass (sh_set_rope's base; 0: none)
+  const float *gq = nullptr, *gk = nullptr;
+  float *dgq = nullptr, *dgk = nullptr;
+  char* scratch = nullptr;             // queries and keys as projected [2, B, H, T, D], then the gradients' workspace; nullptr: forward passes only
+};
+struct ShBalance {                     // sh_set_balance
+  bool on = false;
+  int kind = 0;
+  float coef = 0.f;
+  const void* mask = nullptr;
+  float *loss = nullptr, *prob = nullptr;
+  int* counts = nullptr;
+  const float* gloss = nullptr;
+  char* scratch = nullptr;             // logits [N, G], slope [G], workspace
+};
+struct ShDropout {                     // sh_set_dropout
+  bool on = false;
+  double p = 0.0;
+  const void* rng = nullptr;
+  char* scratch = nullptr;             // the output's gradient behind the mask [N, M]; nullptr: forward passes only
+};
+struct ShTraining { ShQkNorm norm; ShBalance balance; ShDropout dropout; };
+
 struct sh_layer {
   ShDims d{};
+  ShTraining train{};
+  ShTraining fwd_train{};              // as the last forward pass had it (sh_backward differentiates that pass)
   bool dense = false;
   bool moe_q = false, moe_k = false;   // query / key projections are experts too (destination / source side selection)
   bool out_f16 = false;                // sh_set_output_f16: sh_forward writes its result as fp16 (bf16 storage, tensor-core output projection)
@@ -139,6 +168,7 @@ struct sh_layer {
   const void* fwd_x = nullptr;   // input of the forward pass whose intermediates the workspace holds (sh_backward wants the same one); nullptr: none
   int fwd_causal = 1;            // that pass's mask (its row maxima and normalisers belong to it)
   bool rope = false;       // rotary position embeddings on Q, K (table in the workspace)
+  double rope_base = 0.0;
   bool xl_positions = false;   // Transformer-XL relative-position term (fp32 configuration; tables in the workspace)
   int launches = 0;
   int sm_count = 0;
@@ -223,6 +253,9 @@ int sh_simt_run_bf16(sh_layer* L, int stages, const void* x, void* out, cudaStre
 inline int sh_f32_ldz(const ShDims& d) { return (d.G + 31) / 32 * 32; }       // row length of the gate-gradient matrix
 int sh_f32_prepare(sh_layer* L);                // tensor maps, after the weights are split
 void sh_f32_release(sh_layer* L);
+size_t sh_f32_norm_scratch(const sh_layer* L);     // bytes of the scratch of sh_set_qk_norm, sh_set_balance, sh_set_dropout
+size_t sh_f32_balance_scratch(const sh_layer* L);
+size_t sh_f32_dropout_scratch(const sh_layer* L);
 int sh_f32_gate_sort(sh_layer* L, const void* x, cudaStream_t st);
 int sh_f32_forward(sh_layer* L, const void* x, void* out, cudaStream_t st);
 int sh_f32_backward(sh_layer* L, const void* x, const float* dout, float* dx, float* dWq, float* dWk, float* dWv,
@@ -233,6 +266,13 @@ int sh_bf16_gate(sh_layer* L, const void* x, int* blockcnt, bool pdl, cudaStream
 bool sh_bf16_gate_ok(const sh_layer* L);        // its logits fit shared memory (up to about 2000 gate columns)
 // The CUDA-core attention kernel on fp32 storage (the relative-position term of Transformer-XL).
 int sh_simt_attention_f32(sh_layer* L, cudaStream_t st);
+
+// The operators of a training step (sh_train.cu): checks of the arguments and launches; pdl: chained to the kernel before.
+int sh_run_qk_norm(const sh_qk_norm_args& p, bool pdl, cudaStream_t st);
+int sh_run_qk_norm_backward(const sh_qk_norm_backward_args& p, bool pdl, cudaStream_t st);
+int sh_run_balance_loss(const sh_balance_args& p, bool pdl, cudaStream_t st);
+int sh_run_balance_backward(const sh_balance_args& p, bool add, bool pdl, cudaStream_t st);   // add: dlogits += (fp32)
+int sh_run_dropout(const sh_dropout_args& p, bool pdl, cudaStream_t st);
 
 // Tensor-core (tcgen05) path of the bf16 configuration.
 int sh_tc_prepare(sh_layer* L);                 // builds tensor maps after the weights are repacked

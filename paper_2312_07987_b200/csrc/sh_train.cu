@@ -227,10 +227,7 @@ bool bl_aligned(const void* z, long long stride, int gates, int E, int w, int si
   return (uintptr_t)z % bytes == 0 && (tokens < 2 || (size_t)stride * size % bytes == 0) && (gates < 2 || (size_t)E * size % bytes == 0);
 }
 
-int bl_check(const sh_balance_args* p, bool backward) {
-  sh_set_error("%s", "");
-  if (!p) { sh_set_error("args is NULL"); return SH_ERR_INVALID_ARG; }
-  const sh_balance_args& a = *p;
+int bl_check(const sh_balance_args& a, bool backward) {
   if (!dtype_ok(a.dtype, false)) return SH_ERR_INVALID_ARG;
   if (a.n_tokens < 0) { sh_set_error("n_tokens must not be negative (got %lld)", (long long)a.n_tokens); return SH_ERR_INVALID_ARG; }
   if (a.sides < 1 || a.n_heads < 1 || a.n_experts < 1 || a.n_experts > 32) {
@@ -298,41 +295,24 @@ BlPlan bl_plan_for(const sh_balance_args& p, bool backward, int sms) {
 
 }  // namespace
 
-extern "C" int sh_qk_norm(const sh_qk_norm_args* args, void* stream) {
-  sh_set_error("%s", "");
-  if (!args) { sh_set_error("args is NULL"); return SH_ERR_INVALID_ARG; }
-  if (int rc = qn_check(*args, nullptr)) return rc;
-  if (args->batch == 0 || args->seq == 0) return SH_OK;
-  return qn_run(*args, nullptr, false, (cudaStream_t)stream);
+int sh_run_qk_norm(const sh_qk_norm_args& p, bool pdl, cudaStream_t st) {
+  if (int rc = qn_check(p, nullptr)) return rc;
+  if (p.batch == 0 || p.seq == 0) return SH_OK;
+  return qn_run(p, nullptr, pdl, st);
 }
 
-extern "C" size_t sh_qk_norm_workspace_bytes(int d_head) {
-  return d_head < 1 || d_head > QN_MAX_D ? 0 : (size_t)QN_MAX_BLOCKS * d_head * 4;
-}
-
-extern "C" int sh_qk_norm_backward(const sh_qk_norm_backward_args* args, void* stream) {
-  sh_set_error("%s", "");
-  if (!args) { sh_set_error("args is NULL"); return SH_ERR_INVALID_ARG; }
-  const sh_qk_norm_backward_args& a = *args;
-  if (int rc = qn_check(a.norm, args)) return rc;
-  if (a.dgq || a.dgk) {
-    const size_t need = sh_qk_norm_workspace_bytes(a.norm.d_head);
-    if (!a.workspace || (uintptr_t)a.workspace % 256) { sh_set_error("workspace must be a device pointer aligned to 256 bytes"); return SH_ERR_WORKSPACE; }
-    if (a.workspace_bytes < need) { sh_set_error("workspace too small: %zu bytes given, %zu needed", a.workspace_bytes, need); return SH_ERR_WORKSPACE; }
+int sh_run_qk_norm_backward(const sh_qk_norm_backward_args& p, bool pdl, cudaStream_t st) {
+  if (int rc = qn_check(p.norm, &p)) return rc;
+  if (p.dgq || p.dgk) {
+    const size_t need = sh_qk_norm_workspace_bytes(p.norm.d_head);
+    if (!p.workspace || (uintptr_t)p.workspace % 256) { sh_set_error("workspace must be a device pointer aligned to 256 bytes"); return SH_ERR_WORKSPACE; }
+    if (p.workspace_bytes < need) { sh_set_error("workspace too small: %zu bytes given, %zu needed", p.workspace_bytes, need); return SH_ERR_WORKSPACE; }
   }
-  return qn_run(a.norm, args, false, (cudaStream_t)stream);
+  return qn_run(p.norm, &p, pdl, st);
 }
 
-extern "C" size_t sh_balance_workspace_bytes(int sides, int n_heads, int n_experts) {
-  const long long gates = (long long)sides * n_heads;
-  if (sides < 1 || n_heads < 1 || gates > 65535 || n_experts < 1 || n_experts > 32) return 0;
-  return kBlHead + bl_losses(gates) + (size_t)BL_MAX_BLOCKS * (gates * n_experts * 8 + 4);
-}
-
-extern "C" int sh_balance_loss(const sh_balance_args* args, void* stream) {
-  if (int rc = bl_check(args, false)) return rc;
-  const sh_balance_args& p = *args;
-  cudaStream_t st = (cudaStream_t)stream;
+int sh_run_balance_loss(const sh_balance_args& p, bool pdl, cudaStream_t st) {
+  if (int rc = bl_check(p, false)) return rc;
   int sms = 0;
   if (int rc = device_sms(&sms)) return rc;
   const BlPlan pl = bl_plan_for(p, false, sms);
@@ -343,7 +323,7 @@ extern "C" int sh_balance_loss(const sh_balance_args* args, void* stream) {
   a.ticket = (unsigned*)ws;
   a.part_p = (float*)(ws + kBlHead + bl_losses(a.gates));
   a.part_n = (int*)(a.part_p + (size_t)pl.nx * cols);
-  if (int rc = bl_dispatch(p.dtype, a, pl, 0, false, st)) return rc;
+  if (int rc = bl_dispatch(p.dtype, a, pl, 0, pdl, st)) return rc;
   BlOut o;
   o.part_p = a.part_p; o.part_n = a.part_n; o.ticket = a.ticket; o.gate_loss = (double*)(ws + kBlHead);
   o.blocks = pl.nx; o.gates = a.gates; o.E = a.E; o.kind = p.kind; o.coef = p.coef;
@@ -351,22 +331,18 @@ extern "C" int sh_balance_loss(const sh_balance_args* args, void* stream) {
   return launch_k(true, sh_balance_loss_kernel, dim3((unsigned)a.gates), dim3(BL_LOSS_THREADS), 0, st, o);
 }
 
-extern "C" int sh_balance_backward(const sh_balance_args* args, void* stream) {
-  if (int rc = bl_check(args, true)) return rc;
-  const sh_balance_args& p = *args;
+int sh_run_balance_backward(const sh_balance_args& p, bool add, bool pdl, cudaStream_t st) {
+  if (int rc = bl_check(p, true)) return rc;
   if (p.n_tokens == 0) return SH_OK;
   int sms = 0;
   if (int rc = device_sms(&sms)) return rc;
   const BlPlan pl = bl_plan_for(p, true, sms);
   BlArgs a;
   bl_fill(p, pl, a);
-  return bl_dispatch(p.dtype, a, pl, 1, false, (cudaStream_t)stream);
+  return bl_dispatch(p.dtype, a, pl, add ? 2 : 1, pdl, st);
 }
 
-extern "C" int sh_dropout(const sh_dropout_args* args, void* stream) {
-  sh_set_error("%s", "");
-  if (!args) { sh_set_error("args is NULL"); return SH_ERR_INVALID_ARG; }
-  const sh_dropout_args& p = *args;
+int sh_run_dropout(const sh_dropout_args& p, bool pdl, cudaStream_t st) {
   if (!dtype_ok(p.dtype, true)) return SH_ERR_INVALID_ARG;
   if (p.rows < 0 || p.cols < 0) { sh_set_error("rows and cols must not be negative (got %lld, %lld)", (long long)p.rows, (long long)p.cols); return SH_ERR_INVALID_ARG; }
   if (p.rows > (1ll << 32) || p.cols > (1ll << 31) - 8) {
@@ -396,7 +372,7 @@ extern "C" int sh_dropout(const sh_dropout_args* args, void* stream) {
     a.row0 = (unsigned)r; a.units = (unsigned)(n * a.upr);
     const long long blocks = ((long long)a.units + DO_THREADS - 1) / DO_THREADS, cap = 16ll * sms;
     const dim3 grid((unsigned)(blocks < cap ? blocks : cap));
-    auto go = [&](auto kern) { return launch_k(false, kern, grid, dim3(DO_THREADS), 0, (cudaStream_t)stream, a); };
+    auto go = [&](auto kern) { return launch_k(pdl, kern, grid, dim3(DO_THREADS), 0, st, a); };
     auto typed = [&](auto zero) {
       using T = decltype(zero);
       if (p.residual) return vec ? go(sh_dropout_kernel<T, true, true>) : go(sh_dropout_kernel<T, false, true>);
@@ -406,4 +382,38 @@ extern "C" int sh_dropout(const sh_dropout_args* args, void* stream) {
     if (rc) return rc;
   }
   return SH_OK;
+}
+
+extern "C" size_t sh_qk_norm_workspace_bytes(int d_head) {
+  return d_head < 1 || d_head > QN_MAX_D ? 0 : (size_t)QN_MAX_BLOCKS * d_head * 4;
+}
+
+extern "C" size_t sh_balance_workspace_bytes(int sides, int n_heads, int n_experts) {
+  const long long gates = (long long)sides * n_heads;
+  if (sides < 1 || n_heads < 1 || gates > 65535 || n_experts < 1 || n_experts > 32) return 0;
+  return kBlHead + bl_losses(gates) + (size_t)BL_MAX_BLOCKS * (gates * n_experts * 8 + 4);
+}
+
+// An entry point: the reason of the last failure cleared, the struct of arguments given.
+template <typename A, typename F>
+static int entry(const A* args, F run) {
+  sh_set_error("%s", "");
+  if (!args) { sh_set_error("args is NULL"); return SH_ERR_INVALID_ARG; }
+  return run(*args);
+}
+
+extern "C" int sh_qk_norm(const sh_qk_norm_args* args, void* stream) {
+  return entry(args, [&](const sh_qk_norm_args& a) { return sh_run_qk_norm(a, false, (cudaStream_t)stream); });
+}
+extern "C" int sh_qk_norm_backward(const sh_qk_norm_backward_args* args, void* stream) {
+  return entry(args, [&](const sh_qk_norm_backward_args& a) { return sh_run_qk_norm_backward(a, false, (cudaStream_t)stream); });
+}
+extern "C" int sh_balance_loss(const sh_balance_args* args, void* stream) {
+  return entry(args, [&](const sh_balance_args& a) { return sh_run_balance_loss(a, false, (cudaStream_t)stream); });
+}
+extern "C" int sh_balance_backward(const sh_balance_args* args, void* stream) {
+  return entry(args, [&](const sh_balance_args& a) { return sh_run_balance_backward(a, false, false, (cudaStream_t)stream); });
+}
+extern "C" int sh_dropout(const sh_dropout_args* args, void* stream) {
+  return entry(args, [&](const sh_dropout_args& a) { return sh_run_dropout(a, false, (cudaStream_t)stream); });
 }
