@@ -336,7 +336,8 @@ size_t sh_qk_norm_workspace_bytes(int d_head);
  * sh_balance_backward: dlogits = *gloss * dloss/dlogits (gloss: device, NULL: 1), in the type of the logits, tokens
  * dtoken_stride elements apart; the counts are constants of it.  Tokens that do not count get zeros.  Reads logits, mask,
  * slope; dlogits may be logits itself (same stride).
- * workspace: sh_balance_workspace_bytes(sides, H, E) bytes aligned to 256 (sh_balance_loss only).  1 <= k <= E <= 32; N * k
+ * workspace: sh_balance_workspace_bytes(N, sides, H, E) bytes aligned to 256 (sh_balance_loss only; 0: few rows, NULL will do).
+ * 1 <= k <= E <= 32; N * k
  * below 2^31.  The same inputs give the same bits. */
 enum { SH_BALANCE_COUNTS = 0, SH_BALANCE_ENTROPY = 1 };
 typedef struct {
@@ -356,7 +357,7 @@ typedef struct {
 } sh_balance_args;
 int sh_balance_loss(const sh_balance_args* args, void* stream);
 int sh_balance_backward(const sh_balance_args* args, void* stream);
-size_t sh_balance_workspace_bytes(int sides, int n_heads, int n_experts);
+size_t sh_balance_workspace_bytes(int64_t n_tokens, int sides, int n_heads, int n_experts);
 
 /* Dropout: y[r, c] = residual[r, c] + (kept(r, c) ? x[r, c] / (1 - p) : 0) over a matrix of rows x cols (rows x_stride, y_stride,
  * residual_stride elements apart; residual NULL: none).  The mask is never stored: it depends on the seed, the offset, r and c

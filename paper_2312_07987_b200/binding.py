@@ -101,7 +101,7 @@ def _load() -> ctypes.CDLL:
     lib.sh_qk_norm_workspace_bytes.restype = sz
     lib.sh_qk_norm_workspace_bytes.argtypes = [i32]
     lib.sh_balance_workspace_bytes.restype = sz
-    lib.sh_balance_workspace_bytes.argtypes = [i32] * 3
+    lib.sh_balance_workspace_bytes.argtypes = [ctypes.c_int64] + [i32] * 3
     lib.sh_training_scratch_bytes.restype = sz
     lib.sh_training_scratch_bytes.argtypes = [vp, i32]
     lib.sh_set_qk_norm.restype = i32
@@ -446,18 +446,10 @@ def _qk_norm_workspace_bytes(d_head: int) -> int:
     return lib.sh_qk_norm_workspace_bytes(d_head)
 
 
-@functools.lru_cache(maxsize=None)
-def _balance_workspace_bytes(sides: int, heads: int, experts: int) -> int:
-    return lib.sh_balance_workspace_bytes(sides, heads, experts)
-
-
-def _dense(shape: tuple, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
-    """torch.empty (empty_strided skips 1 us of it)."""
-    strides, n = [], 1
-    for s in reversed(shape):
-        strides.append(n)
-        n *= s if s > 1 else 1
-    return torch.empty_strided(shape, strides[::-1], dtype=dtype, device=device)
+@functools.lru_cache(maxsize=4096)
+def _balance_shape(tokens: int, sides: int, heads: int, experts: int):
+    """Shape and strides of a dense [sides, heads, experts], bytes of the workspace."""
+    return (sides, heads, experts), (heads * experts, experts, 1), lib.sh_balance_workspace_bytes(tokens, sides, heads, experts)
 
 
 def sh_qk_norm_backward(q: torch.Tensor, k: Optional[torch.Tensor], dq: torch.Tensor, dk: Optional[torch.Tensor], gq: Optional[torch.Tensor] = None,
@@ -473,7 +465,7 @@ def sh_qk_norm_backward(q: torch.Tensor, k: Optional[torch.Tensor], dq: torch.Te
     ws, nbytes = None, 0
     if gq is not None or gk is not None:
         nbytes = _qk_norm_workspace_bytes(q.shape[3])
-        ws = _dense((nbytes,), torch.uint8, q.device)
+        ws = torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=q.device)     # (1 us less than torch.empty)
     _launch(lib.sh_qk_norm_backward, _QK_NORM_BACKWARD.pack(*fields, *_heads("dq", dq, q, q.shape), *(_NO_HEADS if k is None else _heads("dk", dk, q, k.shape)),
                                                             0 if dgq is None else dgq.data_ptr(), 0 if dgk is None else dgk.data_ptr(),
                                                             0 if ws is None else ws.data_ptr(), nbytes), q.get_device())
@@ -507,14 +499,14 @@ def sh_balance_loss(logits: torch.Tensor, idx: torch.Tensor, *, kind: str = "cou
     if kind not in SH_BALANCE:
         raise ValueError(f"kind must be one of {sorted(SH_BALANCE)}: got {kind!r}")
     dev = logits.device
-    loss = _dense((), torch.float32, dev)
-    prob = _dense((S, H, E), torch.float32, dev)
+    shape, strides, nbytes = _balance_shape(N, S, H, E)
+    loss = torch.empty_strided((), (), dtype=torch.float32, device=dev)
+    prob = torch.empty_strided(shape, strides, dtype=torch.float32, device=dev)
     slope = torch.empty_like(prob)
     counts = torch.empty_like(prob, dtype=torch.int32)
-    nbytes = _balance_workspace_bytes(S, H, E)
-    ws = _dense((nbytes,), torch.uint8, dev)
+    ws = torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=dev) if nbytes else None
     _launch(lib.sh_balance_loss, _BALANCE.pack(N, logits.stride(0), 0, logits.data_ptr(), idx.data_ptr(), _token_mask(mask, logits), 0, loss.data_ptr(),
-                                               prob.data_ptr(), slope.data_ptr(), counts.data_ptr(), 0, ws.data_ptr(), nbytes,
+                                               prob.data_ptr(), slope.data_ptr(), counts.data_ptr(), 0, ws.data_ptr() if nbytes else 0, nbytes,
                                                _DTYPES[logits.dtype], SH_BALANCE[kind], S, H, E, idx.shape[3], coef, 0), logits.get_device())
     return dict(loss=loss, counts=counts, prob=prob, slope=slope)
 

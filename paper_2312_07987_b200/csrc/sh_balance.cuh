@@ -7,9 +7,11 @@
 // A row (a token's E logits of one gate) belongs to L neighbouring lanes with W values each.  Between its rounds a thread
 // stays with the same gate, so its share of P is W sums in registers.
 #pragma once
+#include <cooperative_groups.h>
+
 #include "sh_vec.cuh"
 
-constexpr int BL_THREADS = 256;
+constexpr int BL_THREADS = 256, BL_BLOCKS = 3;     // (two rows a thread on their way, 24 warps an SM: 16 warps 5 % slower, more rows the same)
 constexpr int BL_LOSS_THREADS = 512;
 constexpr int BL_MAX_BLOCKS = 512;         // blocks of the first kernel at most (rows of partial results)
 
@@ -88,62 +90,72 @@ __device__ __forceinline__ float bl_softmax(float2 (&f)[W / 2]) {
   return s == 0.f ? 0.f : __fdividef(1.f, s);
 }
 
-// A block's share of the sums: tokens tpb at a time, blockIdx.y's gates.
-template <typename T, int W, int L, bool VEC>
-static __global__ void __launch_bounds__(BL_THREADS, 3) sh_balance_sums_kernel(const BlArgs a) {
-  constexpr int EP = W * L, ROWS = BL_THREADS / L, AHEAD = BlAhead<T, W>::N, PICKS = 4 / L < 1 ? 1 : 4 / L;
-  __shared__ float s_p[ROWS][EP + 1];
-  __shared__ int s_n[ROWS * EP];                         // [gate of the block][expert]
-  __shared__ int s_tokens;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+// A block's share of the sums, tokens tpb at a time from its place among `blocks` blocks on, gates g0 .. g0 + ng - 1: into s_p a row of
+// the block's sums of p, into s_n the counts (both cleared or overwritten here), into *s_tokens the tokens that count.
+template <typename T, int W, int L, bool VEC, int THREADS>
+__device__ __forceinline__ void bl_sums(const BlArgs& a, int block, int blocks, int g0, int ng, float (*s_p)[W * L + 1], int* s_n, int* s_tokens) {
+  constexpr int EP = W * L, AHEAD = BlAhead<T, W>::N, PICKS = 4 / L < 1 ? 1 : 4 / L;
   const int row = threadIdx.x / L, sub = threadIdx.x % L, at = sub * W;
-  const int g0 = blockIdx.y * a.per, ng = min(a.per, a.gates - g0);
   const int gl = row % a.per, tl = row / a.per, gate = g0 + gl;
   const bool mine = tl < a.tpb && gl < ng;
-  for (int i = threadIdx.x; i < ng * EP; i += BL_THREADS) s_n[i] = 0;
-  if (threadIdx.x == 0) s_tokens = 0;
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.ticket = 0;
+  for (int i = threadIdx.x; i < ng * EP; i += THREADS) s_n[i] = 0;
+  if (threadIdx.x == 0) *s_tokens = 0;
   __syncthreads();
   float2 acc[W / 2];
 #pragma unroll
   for (int i = 0; i < W / 2; ++i) acc[i] = make_float2(0.f, 0.f);
   int seen = 0;
   auto count = [&](int e) { if ((unsigned)e < (unsigned)a.E) atomicAdd(&s_n[gl * EP + e], 1); };   // (a slot without an expert is not counted)
-  const long long step = (long long)gridDim.x * a.tpb;
-  long long t = (long long)blockIdx.x * a.tpb + tl;      // (what is past the last token is not read)
+  const long long step = (long long)blocks * a.tpb;
+  long long t = (long long)block * a.tpb + tl;           // (what is past the last token is not read)
   const T* z = (const T*)a.z + (long long)gate * a.E + at + t * a.zt;
   const int* idx = a.idx + ((long long)(gate / a.H) * a.tokens * a.H + gate % a.H + t * a.H) * a.k;
-  const long long zstep = step * a.zt, istep = step * a.H * a.k, rounds = (a.tokens - (long long)blockIdx.x * a.tpb + step - 1) / step;
+  const long long zstep = step * a.zt, istep = step * a.H * a.k, rounds = (a.tokens - (long long)block * a.tpb + step - 1) / step;
+  // (the next AHEAD rows are on their way while one is worked on)
+  BlRow<T, W, VEC> rows[AHEAD];
+  int picks[AHEAD][PICKS];
+  auto fetch = [&](int u) {
+    const bool live = mine && t < a.tokens && (!a.mask || a.mask[t]);
+    rows[u].load(z, a.E - at, live);
+#pragma unroll
+    for (int j = 0; j < PICKS; ++j) picks[u][j] = live && sub * PICKS + j < a.k ? __ldcs(idx + sub * PICKS + j) : -1;
+    if (live)
+      for (int j = L * PICKS + sub; j < a.k; j += L) count(__ldcs(idx + j));
+    seen += live;
+    t += step; z += zstep; idx += istep;
+  };
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u) fetch(u);
   for (long long r = 0; r < rounds; r += AHEAD) {
-    BlRow<T, W, VEC> rows[AHEAD];
-    int picks[AHEAD][PICKS];
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
-      const bool live = mine && t < a.tokens && (!a.mask || a.mask[t]);
-      rows[u].load(z, a.E - at, live);
-#pragma unroll
-      for (int j = 0; j < PICKS; ++j) picks[u][j] = live && sub * PICKS + j < a.k ? __ldcs(idx + sub * PICKS + j) : -1;
-      if (live)
-        for (int j = L * PICKS + sub; j < a.k; j += L) count(__ldcs(idx + j));
-      seen += live;
-      t += step; z += zstep; idx += istep;
-    }
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-#pragma unroll
-      for (int j = 0; j < PICKS; ++j) count(picks[u][j]);
       float2 f[W / 2];
       rows[u].get(f);
+#pragma unroll
+      for (int j = 0; j < PICKS; ++j) count(picks[u][j]);
+      fetch(u);
       const float inv = bl_softmax<W, L>(f);
 #pragma unroll
       for (int i = 0; i < W / 2; ++i) acc[i] = __ffma2_rn(f[i], make_float2(inv, inv), acc[i]);
     }
   }
-  if (mine && gl == 0 && sub == 0 && seen) atomicAdd(&s_tokens, seen);
+  if (mine && gl == 0 && sub == 0 && seen) atomicAdd(s_tokens, seen);
 #pragma unroll
   for (int i = 0; i < W / 2; ++i) { s_p[row][at + 2 * i] = acc[i].x; s_p[row][at + 2 * i + 1] = acc[i].y; }
   __syncthreads();
+}
+
+template <typename T, int W, int L, bool VEC>
+static __global__ void __launch_bounds__(BL_THREADS, BL_BLOCKS) sh_balance_sums_kernel(const BlArgs a) {
+  constexpr int EP = W * L, ROWS = BL_THREADS / L;
+  __shared__ float s_p[ROWS][EP + 1];
+  __shared__ int s_n[ROWS * EP];                         // [gate of the block][expert]
+  __shared__ int s_tokens;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.ticket = 0;
+  const int g0 = blockIdx.y * a.per, ng = min(a.per, a.gates - g0);
+  bl_sums<T, W, L, VEC, BL_THREADS>(a, blockIdx.x, gridDim.x, g0, ng, s_p, s_n, &s_tokens);
   const long long base = (long long)blockIdx.x * a.gates * a.E;
   for (int i = threadIdx.x; i < ng * a.E; i += BL_THREADS) {
     const int q = i / a.E, e = i % a.E;
@@ -162,8 +174,37 @@ struct BlOut {
   float *loss, *prob, *slope; int* counts;
 };
 
-// A gate per block: its experts' sums over the first kernel's blocks in a fixed order, in 64 bits, its share of the loss
-// and the centred slope; the block that comes last adds the gates' losses in order.
+// A gate's results from its sums: lane e of a warp has expert e's sum of p and count; in 64 bits.  Returns its share of the loss.
+__device__ __forceinline__ double bl_finish(const BlOut& a, int gate, int e, double p, int n, int tokens) {
+  const double P = tokens ? p / tokens : 0.0;
+  int all = n;
+  for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+  const double f = all ? (double)n / all : 0.0;
+  // (an expert without any probability has no slope: p is zero wherever it would be used)
+  const bool used = e < a.E && (a.kind == 0 || P != 0.0);
+  double c = 0.0, l = 0.0;
+  if (used) {
+    if (a.kind == 0) { l = a.E * f * P; c = a.E * f; }
+    else { c = log(P); l = P * c; }
+  }
+  double sum = c;
+  int many = used;
+  for (int o = 16; o > 0; o >>= 1) {
+    l += __shfl_xor_sync(0xffffffffu, l, o);
+    sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    many += __shfl_xor_sync(0xffffffffu, many, o);
+  }
+  if (e < a.E) {
+    const int o = gate * a.E + e;
+    a.counts[o] = n;
+    a.prob[o] = (float)P;
+    a.slope[o] = used && tokens ? (float)(a.coef * (c - sum / many) / tokens) : 0.f;
+  }
+  return tokens ? a.coef * l : 0.0;
+}
+
+// A gate per block: its experts' sums over the first kernel's blocks in a fixed order; the block that comes last adds the gates'
+// losses in order.
 static __global__ void __launch_bounds__(BL_LOSS_THREADS) sh_balance_loss_kernel(const BlOut a) {
   constexpr int ROWS = BL_LOSS_THREADS / 32;
   __shared__ double s_p[ROWS][32];
@@ -191,35 +232,11 @@ static __global__ void __launch_bounds__(BL_LOSS_THREADS) sh_balance_loss_kernel
   if (e == 0) s_t[r] = tokens;
   __syncthreads();
   if (r == 0) {
-    tokens = 0;
-    for (int i = 0; i < ROWS; ++i) { tokens += s_t[i]; if (i) { p += s_p[i][e]; n += s_n[i][e]; } }
-    const double P = tokens ? p / tokens : 0.0;
-    int all = n;
-    for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
-    const double f = all ? (double)n / all : 0.0;
-    // (an expert without any probability has no slope: p is zero wherever it would be used)
-    double c = 0.0, l = 0.0, mean = 0.0;
-    if (e < a.E) {
-      if (a.kind == 0) { l = a.E * f * P; c = a.E * f; }
-      else if (P != 0.0) { c = log(P); l = P * c; }
-    }
-    const int used = a.kind == 0 || P != 0.0;
-    double cs = e < a.E && used ? c : 0.0;
-    int cn = e < a.E && used;
-    for (int o = 16; o > 0; o >>= 1) {
-      l += __shfl_xor_sync(0xffffffffu, l, o);
-      cs += __shfl_xor_sync(0xffffffffu, cs, o);
-      cn += __shfl_xor_sync(0xffffffffu, cn, o);
-    }
-    mean = cn ? cs / cn : 0.0;
-    if (e < a.E) {
-      const int o = gate * a.E + e;
-      a.counts[o] = n;
-      a.prob[o] = (float)P;
-      a.slope[o] = used && tokens ? (float)(a.coef * (c - mean) / tokens) : 0.f;
-    }
+    tokens = s_t[0];
+    for (int i = 1; i < ROWS; ++i) { tokens += s_t[i]; p += s_p[i][e]; n += s_n[i][e]; }
+    const double l = bl_finish(a, gate, e, p, n, tokens);
     if (e == 0) {
-      a.gate_loss[gate] = tokens ? a.coef * l : 0.0;
+      a.gate_loss[gate] = l;
       __threadfence();
       s_last = atomicAdd(a.ticket, 1u) == (unsigned)a.gates - 1;
     }
@@ -233,9 +250,57 @@ static __global__ void __launch_bounds__(BL_LOSS_THREADS) sh_balance_loss_kernel
   }
 }
 
+// Both in one launch, for few rows: a cluster of 8 blocks, whose sums are read over distributed shared memory, a warp to a gate.
+// (Such calls are bound by their launches: 2048 tokens, 8 gates of 4 experts, 13.8 us a call, 17.4 with the two kernels.)
+constexpr int BL_SMALL_THREADS = 512, BL_CLUSTER = 8;
+constexpr int BL_SMALL_COLS = 1024, BL_SMALL_GATES = 64;   // gates * experts, gates at most
+template <typename T, int W, int L, bool VEC>
+static __global__ void __launch_bounds__(BL_SMALL_THREADS, 1) sh_balance_small_kernel(const BlArgs a, const BlOut o) {
+  namespace cg = cooperative_groups;
+  constexpr int EP = W * L, ROWS = BL_SMALL_THREADS / L;
+  __shared__ float s_p[ROWS][EP + 1];
+  __shared__ int s_n[BL_SMALL_GATES * EP < 2 * BL_SMALL_COLS ? BL_SMALL_GATES * EP : 2 * BL_SMALL_COLS];
+  __shared__ float s_sum[BL_SMALL_COLS];
+  __shared__ double s_loss[BL_SMALL_GATES];
+  __shared__ int s_tokens;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = (int)cluster.block_rank();
+  bl_sums<T, W, L, VEC, BL_SMALL_THREADS>(a, rank, BL_CLUSTER, 0, a.gates, s_p, s_n, &s_tokens);
+  for (int i = threadIdx.x; i < a.gates * a.E; i += BL_SMALL_THREADS) {
+    const int q = i / a.E, e = i % a.E;
+    float sum = 0.f;
+    for (int k = 0; k < a.tpb; ++k) sum += s_p[k * a.per + q][e];
+    s_sum[i] = sum;
+  }
+  cluster.sync();
+  const int e = threadIdx.x & 31;
+  for (int gate = rank + BL_CLUSTER * (threadIdx.x >> 5); gate < a.gates; gate += BL_CLUSTER * (BL_SMALL_THREADS / 32)) {
+    double p = 0.0;
+    int n = 0, tokens = 0;
+#pragma unroll
+    for (int b = 0; b < BL_CLUSTER; ++b) {
+      if (e < a.E) {
+        p += (double)cluster.map_shared_rank(s_sum, b)[gate * a.E + e];
+        n += cluster.map_shared_rank(s_n, b)[gate * EP + e];
+      }
+      tokens += *cluster.map_shared_rank(&s_tokens, b);
+    }
+    const double l = bl_finish(o, gate, e, p, n, tokens);
+    if (e == 0) cluster.map_shared_rank(s_loss, 0)[gate] = l;
+  }
+  cluster.sync();                                        // (nobody's shared memory is read behind it)
+  if (rank == 0 && threadIdx.x == 0) {
+    double sum = 0.0;
+    for (int i = 0; i < a.gates; ++i) sum += s_loss[i];
+    *o.loss = (float)sum;
+  }
+}
+
 // dz, or dz += (ADD: fp32, the gates' gradients of a backward pass).
 template <typename T, int W, int L, bool VEC, bool ADD>
-static __global__ void __launch_bounds__(BL_THREADS, 3) sh_balance_backward_kernel(const BlArgs a) {
+static __global__ void __launch_bounds__(BL_THREADS, BL_BLOCKS) sh_balance_backward_kernel(const BlArgs a) {
   constexpr int AHEAD = BlAhead<T, W>::N;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -251,20 +316,23 @@ static __global__ void __launch_bounds__(BL_THREADS, 3) sh_balance_backward_kern
   const T* z = (const T*)a.z + (long long)gate * a.E + at + t * a.zt;
   T* o = (T*)a.dz + (long long)gate * a.E + at + t * a.dzt;
   const long long zstep = step * a.zt, ostep = step * a.dzt, rounds = (a.tokens - (long long)blockIdx.x * a.tpb + step - 1) / step;
-  for (long long r = 0; r < rounds; r += AHEAD) {
-    BlRow<T, W, VEC> rows[AHEAD];
-    bool there[AHEAD], live[AHEAD];
+  BlRow<T, W, VEC> rows[AHEAD];
+  bool there[AHEAD], live[AHEAD];
+  auto fetch = [&](int u) {
+    there[u] = mine && t < a.tokens;
+    live[u] = there[u] && (!a.mask || a.mask[t]);
+    rows[u].load(z, a.E - at, live[u]);
+    t += step; z += zstep;
+  };
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      there[u] = mine && t < a.tokens;
-      live[u] = there[u] && (!a.mask || a.mask[t]);
-      rows[u].load(z, a.E - at, live[u]);
-      t += step; z += zstep;
-    }
+  for (int u = 0; u < AHEAD; ++u) fetch(u);
+  for (long long r = 0; r < rounds; r += AHEAD) {
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       float2 f[W / 2];
       rows[u].get(f);
+      const bool row = there[u], counts = live[u];
+      fetch(u);
       const float inv = bl_softmax<W, L>(f);
       float2 d2 = make_float2(0.f, 0.f);
 #pragma unroll
@@ -278,12 +346,12 @@ static __global__ void __launch_bounds__(BL_THREADS, 3) sh_balance_backward_kern
 #pragma unroll
       for (int i = 0; i < W / 2; ++i) {
         const float2 v = __fmul2_rn(__fmul2_rn(f[i], make_float2(by, by)), __fadd2_rn(c[i], make_float2(dot, dot)));
-        g[2 * i] = live[u] ? v.x : 0.f; g[2 * i + 1] = live[u] ? v.y : 0.f;
+        g[2 * i] = counts ? v.x : 0.f; g[2 * i + 1] = counts ? v.y : 0.f;
       }
-      if (there[u]) {
+      if (row) {
         if constexpr (ADD) {
 #pragma unroll
-          for (int i = 0; i < W; ++i) if (live[u] && at + i < a.E) o[i] += g[i];
+          for (int i = 0; i < W; ++i) if (counts && at + i < a.E) o[i] += g[i];
         } else if constexpr (VEC) {
           sh_store<T, W>(o, g);
         } else {

@@ -13,9 +13,12 @@ struct DoArgs {
   long long xs, rs, ys;                    // row strides
   unsigned row0, units;                    // first row of this launch; pieces of 8 columns in it
   unsigned upr;                            // pieces in a row
-  int cols, limit;
+  int cols, none;                          // none: nothing is kept
+  unsigned limit;                          // what 16 bits in the upper half of a word are compared with
   float scale;
 };
+// DENSE: whole pieces one behind the other; VECTORS: rows keep 16-byte alignment, a row may end inside a piece; VALUES: anything.
+enum { DO_DENSE = 0, DO_VECTORS = 1, DO_VALUES = 2 };
 
 struct ShPhiloxKey { unsigned k[20]; };     // the keys of the ten rounds
 __device__ __forceinline__ ShPhiloxKey sh_philox_key(unsigned long long seed) {
@@ -33,68 +36,71 @@ __device__ __forceinline__ uint4 sh_philox(uint4 c, const ShPhiloxKey& key) {
   return c;
 }
 
-// A thread takes 8 neighbouring columns, one counter, and two such pieces at a time.  VEC: rows of x, residual and y keep
-// 16-byte alignment.
-template <typename T, bool VEC, bool RES>
+// A thread takes pieces of 8 neighbouring columns, one counter each; the next two are on their way while one is worked on.
+// The generator is what costs: 20 wide multiplications and as many three-way ors a piece, so its 128 bits serve 8 values, and what
+// is left of the work - two operations, a comparison and a selection a value - is kept off addresses.
+template <typename T, int MODE, bool RES>
 static __global__ void __launch_bounds__(DO_THREADS) sh_dropout_kernel(const DoArgs a) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const unsigned long long seed = __ldg(a.rng), offset = __ldg(a.rng + 1);
-  const ShPhiloxKey key = sh_philox_key(seed);
   const unsigned step = gridDim.x * DO_THREADS, step_r = step / a.upr, step_b = step - step_r * a.upr;
-  unsigned u = blockIdx.x * DO_THREADS + threadIdx.x, r = u / a.upr, blk = u - r * a.upr;
-  const bool all = a.limit > 65535;                      // nothing is kept
-  const unsigned limit = (unsigned)a.limit << 16;
+  unsigned u = blockIdx.x * DO_THREADS + threadIdx.x, r = u / a.upr, blk = u - r * a.upr;     // of the piece that is worked on
   constexpr int AHEAD = 2;
-  while (u < a.units) {
-    ShRaw<T, 8> x[AHEAD], res[AHEAD];
-    unsigned rows[AHEAD], blks[AHEAD];
-    bool there[AHEAD];
+  unsigned fu = u, fr = r, fb = blk;                     // of the piece that is fetched
+  ShRaw<T, 8> x[AHEAD], res[AHEAD];
+  auto next = [&](unsigned& pu, unsigned& pr, unsigned& pb) {
+    pu += step;
+    pr += step_r; pb += step_b;
+    if (pb >= a.upr) { pb -= a.upr; ++pr; }
+  };
+  auto fetch = [&](int q) {
+    if (fu < a.units) {
+      const long long at = MODE == DO_DENSE ? (long long)fu * 8 : (long long)fr * a.xs + (long long)fb * 8;
+      const T* px = (const T*)a.x + at;
+      const T* pr = RES ? (const T*)a.residual + (MODE == DO_DENSE ? at : (long long)fr * a.rs + (long long)fb * 8) : nullptr;
+      const int n = a.cols - (int)fb * 8;
+      if (MODE == DO_DENSE || (MODE == DO_VECTORS && n >= 8)) {
+        x[q].load(px);
+        if constexpr (RES) res[q].load(pr);
+      } else {
 #pragma unroll
-    for (int q = 0; q < AHEAD; ++q) {
-      there[q] = u < a.units;
-      rows[q] = r; blks[q] = blk;
-      if (there[q]) {
-        const long long row = (long long)a.row0 + r;
-        const T* px = (const T*)a.x + row * a.xs + (long long)blk * 8;
-        const T* pr = RES ? (const T*)a.residual + row * a.rs + (long long)blk * 8 : nullptr;
-        const int n = a.cols - (int)blk * 8;
-        if (VEC && n >= 8) {
-          x[q].load(px);
-          if constexpr (RES) res[q].load(pr);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            reinterpret_cast<T*>(x[q].w)[i] = i < n ? px[i] : T(0.f);
-            if constexpr (RES) reinterpret_cast<T*>(res[q].w)[i] = i < n ? pr[i] : T(0.f);
-          }
+        for (int i = 0; i < 8; ++i) {
+          reinterpret_cast<T*>(x[q].w)[i] = i < n ? px[i] : T(0.f);
+          if constexpr (RES) reinterpret_cast<T*>(res[q].w)[i] = i < n ? pr[i] : T(0.f);
         }
       }
-      u += step; r += step_r; blk += step_b;
-      if (blk >= a.upr) { blk -= a.upr; ++r; }
     }
+    if constexpr (MODE == DO_DENSE) fu += step;
+    else next(fu, fr, fb);
+  };
+#pragma unroll
+  for (int q = 0; q < AHEAD; ++q) fetch(q);
+  const ShPhiloxKey key = sh_philox_key(seed);
+  while (u < a.units) {
 #pragma unroll
     for (int q = 0; q < AHEAD; ++q) {
-      if (!there[q]) break;
-      const unsigned row = a.row0 + rows[q];
-      const uint4 w = sh_philox(make_uint4(blks[q], row, (unsigned)offset, (unsigned)(offset >> 32)), key);
+      if (u >= a.units) break;
+      const uint4 w = sh_philox(make_uint4(blk, a.row0 + r, (unsigned)offset, (unsigned)(offset >> 32)), key);
       const unsigned bits[4] = {w.x, w.y, w.z, w.w};
       float f[8], add[8];
       x[q].get(f);
       if constexpr (RES) res[q].get(add);
+      fetch(q);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         // (the value's 16 bits in the upper half of a word; a dropped value does not count, whatever it is)
         const unsigned v = i & 1 ? bits[i / 2] : bits[i / 2] << 16;
-        const float d = !all && v >= limit ? f[i] * a.scale : 0.f;
+        const float d = v >= a.limit && !a.none ? f[i] * a.scale : 0.f;
         f[i] = RES ? d + add[i] : d;
       }
-      T* y = (T*)a.y + (long long)row * a.ys + (long long)blks[q] * 8;
-      const int n = a.cols - (int)blks[q] * 8;
-      if (VEC && n >= 8) sh_store<T, 8>(y, f);
+      T* y = (T*)a.y + (MODE == DO_DENSE ? (long long)u * 8 : (long long)r * a.ys + (long long)blk * 8);
+      const int n = a.cols - (int)blk * 8;
+      if (MODE == DO_DENSE || (MODE == DO_VECTORS && n >= 8)) sh_store<T, 8>(y, f);
       else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) if (i < n) y[i] = sh_from_float<T>(f[i]);
       }
+      next(u, r, blk);
     }
   }
 }

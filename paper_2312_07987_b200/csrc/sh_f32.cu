@@ -303,7 +303,7 @@ sh_balance_args balance_args(sh_layer* L, const ShBalance& b) {
   a.loss = b.loss; a.prob = b.prob; a.counts = b.counts;
   const size_t logits = up256((size_t)d.N * d.G * 4), slope = up256((size_t)d.G * 4);
   a.slope = (float*)(b.scratch + logits);
-  a.workspace = b.scratch + logits + slope; a.workspace_bytes = sh_balance_workspace_bytes(d.sides, d.H, d.E);
+  a.workspace = b.scratch + logits + slope; a.workspace_bytes = sh_balance_workspace_bytes(d.N, d.sides, d.H, d.E);
   a.dtype = SH_F32; a.kind = b.kind; a.sides = d.sides; a.n_heads = d.H; a.n_experts = d.E; a.k = d.k; a.coef = b.coef;
   return a;
 }
@@ -384,7 +384,7 @@ int sh_f32_prepare(sh_layer* L) {
 size_t sh_f32_norm_scratch(const sh_layer* L) { return up256(2 * raw_heads(L->d) * 4) + sh_qk_norm_workspace_bytes(L->d.Dt); }
 size_t sh_f32_balance_scratch(const sh_layer* L) {
   const ShDims& d = L->d;
-  return up256((size_t)d.N * d.G * 4) + up256((size_t)d.G * 4) + sh_balance_workspace_bytes(d.sides, d.H, d.E);
+  return up256((size_t)d.N * d.G * 4) + up256((size_t)d.G * 4) + sh_balance_workspace_bytes(d.N, d.sides, d.H, d.E);
 }
 size_t sh_f32_dropout_scratch(const sh_layer* L) { return (size_t)sh_out_rows(L->d) * L->d.M * 4; }
 
@@ -429,7 +429,7 @@ int sh_f32_forward(sh_layer* L, const void* x, void* out, cudaStream_t st) {
   if ((rc = launch_gate_sort(L, x, v, nhd, st, tr.balance.on ? (float*)tr.balance.scratch : nullptr))) return rc;
   if (tr.balance.on) {
     if ((rc = sh_run_balance_loss(balance_args(L, tr.balance), chained(L), st))) return rc;
-    L->launches += 2;
+    L->launches += sh_balance_workspace_bytes(d.N, d.sides, d.H, d.E) ? 2 : 1;
   }
   sh_mark(L, 1, st);
   if (L->ev && (rc = launch_x<X_QK>(L, st, qk))) return rc;

@@ -59,7 +59,7 @@ def test_norm_of_no_rows_needs_no_device():
 
 
 def balance_args(**kw):
-    f = dict(n_tokens=8, token_stride=16, dtoken_stride=16, logits=PTR, idx=PTR, mask=0, gloss=0, loss=PTR, prob=PTR, slope=PTR, counts=PTR, dlogits=PTR, workspace=PTR,
+    f = dict(n_tokens=1 << 20, token_stride=16, dtoken_stride=16, logits=PTR, idx=PTR, mask=0, gloss=0, loss=PTR, prob=PTR, slope=PTR, counts=PTR, dlogits=PTR, workspace=PTR,
              workspace_bytes=1 << 30, dtype=b.SH_F32, kind=0, sides=2, n_heads=2, n_experts=4, k=2, coef=1.0, reserved=0)
     f.update(kw)
     return b._BALANCE.pack(*[f[n] for n in BALANCE])
@@ -83,8 +83,10 @@ def test_balance_backward_refusals(kw, frag):
 
 
 def test_balance_workspace():
-    assert b.lib.sh_balance_workspace_bytes(2, 8, 16) > b.lib.sh_balance_workspace_bytes(2, 2, 4) > 0
-    assert b.lib.sh_balance_workspace_bytes(0, 8, 16) == 0 and b.lib.sh_balance_workspace_bytes(1, 1, 33) == 0
+    need = lambda n, *a: b.lib.sh_balance_workspace_bytes(n, *a)
+    assert need(1 << 20, 2, 8, 16) > need(1 << 20, 2, 2, 4) > 0 and need(1, 2, 40, 32) > 0
+    assert need(1, 2, 2, 4) == 0                            # few rows: one launch without a workspace
+    assert need(8, 0, 8, 16) == 0 and need(8, 1, 1, 33) == 0
 
 
 @pytest.mark.parametrize("kw,code,frag", [
