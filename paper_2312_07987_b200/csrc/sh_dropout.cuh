@@ -14,11 +14,15 @@ struct DoArgs {
   unsigned row0, units;                    // first row of this launch; pieces of 8 columns in it
   unsigned upr;                            // pieces in a row
   int cols, none;                          // none: nothing is kept
+  int group_log;                           // rows at any address: lanes to a segment of a row, as a power of two
+  unsigned segs, groups;                   // ... segments of a row, and of the launch
+  long long values;                        // dense rows of any length: of the launch (units: pieces of 16)
   unsigned limit;                          // what 16 bits in the upper half of a word are compared with
   float scale;
 };
-// DENSE: whole pieces one behind the other; VECTORS: rows keep 16-byte alignment, a row may end inside a piece; VALUES: anything.
-enum { DO_DENSE = 0, DO_VECTORS = 1, DO_VALUES = 2 };
+// DENSE: whole pieces one behind the other; VECTORS: rows keep 16-byte alignment, a row may end inside a piece.  (Other
+// rows: sh_dropout_flat_kernel, sh_dropout_rows_kernel.)
+enum { DO_DENSE = 0, DO_VECTORS = 1 };
 
 struct ShPhiloxKey { unsigned k[20]; };     // the keys of the ten rounds
 __device__ __forceinline__ ShPhiloxKey sh_philox_key(unsigned long long seed) {
@@ -34,6 +38,30 @@ __device__ __forceinline__ uint4 sh_philox(uint4 c, const ShPhiloxKey& key) {
     c = make_uint4((unsigned)(b >> 32) ^ c.y ^ key.k[2 * i], (unsigned)b, (unsigned)(a >> 32) ^ c.w ^ key.k[2 * i + 1], (unsigned)a);
   }
   return c;
+}
+
+// N values behind their mask, in place: value i's 16 bits are half i of the words.
+template <bool RES, int N>
+__device__ __forceinline__ void sh_dropout_values(const DoArgs& a, const unsigned (&bits)[N / 2], float (&f)[N], const float (&add)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    // (the 16 bits in the upper half of a word; a dropped value does not count, whatever it is)
+    const unsigned v = i & 1 ? bits[i / 2] : bits[i / 2] << 16;
+    const float d = v >= a.limit && !a.none ? f[i] * a.scale : 0.f;
+    f[i] = RES ? d + add[i] : d;
+  }
+}
+// The 8 halves of piece blk of row r.
+__device__ __forceinline__ void sh_dropout_bits(const ShPhiloxKey& key, unsigned long long offset, unsigned row, unsigned blk, unsigned* bits) {
+  const uint4 w = sh_philox(make_uint4(blk, row, (unsigned)offset, (unsigned)(offset >> 32)), key);
+  bits[0] = w.x; bits[1] = w.y; bits[2] = w.z; bits[3] = w.w;
+}
+// Piece blk of row r behind its mask, in place.
+template <bool RES>
+__device__ __forceinline__ void sh_dropout_piece(const DoArgs& a, const ShPhiloxKey& key, unsigned long long offset, unsigned r, unsigned blk, float (&f)[8], const float (&add)[8]) {
+  unsigned bits[4];
+  sh_dropout_bits(key, offset, a.row0 + r, blk, bits);
+  sh_dropout_values<RES, 8>(a, bits, f, add);
 }
 
 // A thread takes pieces of 8 neighbouring columns, one counter each; the next two are on their way while one is worked on.
@@ -80,19 +108,11 @@ static __global__ void __launch_bounds__(DO_THREADS) sh_dropout_kernel(const DoA
 #pragma unroll
     for (int q = 0; q < AHEAD; ++q) {
       if (u >= a.units) break;
-      const uint4 w = sh_philox(make_uint4(blk, a.row0 + r, (unsigned)offset, (unsigned)(offset >> 32)), key);
-      const unsigned bits[4] = {w.x, w.y, w.z, w.w};
       float f[8], add[8];
       x[q].get(f);
       if constexpr (RES) res[q].get(add);
       fetch(q);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        // (the value's 16 bits in the upper half of a word; a dropped value does not count, whatever it is)
-        const unsigned v = i & 1 ? bits[i / 2] : bits[i / 2] << 16;
-        const float d = v >= a.limit && !a.none ? f[i] * a.scale : 0.f;
-        f[i] = RES ? d + add[i] : d;
-      }
+      sh_dropout_piece<RES>(a, key, offset, r, blk, f, add);
       T* y = (T*)a.y + (MODE == DO_DENSE ? (long long)u * 8 : (long long)r * a.ys + (long long)blk * 8);
       const int n = a.cols - (int)blk * 8;
       if (MODE == DO_DENSE || (MODE == DO_VECTORS && n >= 8)) sh_store<T, 8>(y, f);
@@ -102,5 +122,141 @@ static __global__ void __launch_bounds__(DO_THREADS) sh_dropout_kernel(const DoA
       }
       next(u, r, blk);
     }
+  }
+}
+
+// Dense rows of any length from 16 columns on: a thread takes 16 values one behind the other, which begin anywhere in a piece and
+// may end in the next row.  Their bits are those of three pieces, shifted to the first value by its place in its piece (and, where the
+// row ends, those of two of the next row, shifted the other way).  16384 x 2001 in bf16: ... us; with 8 columns a thread, whose values lie at
+// no vector's address, 91.
+template <typename T, bool RES>
+static __global__ void __launch_bounds__(DO_THREADS) sh_dropout_flat_kernel(const DoArgs a) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const unsigned long long seed = __ldg(a.rng), offset = __ldg(a.rng + 1);
+  const unsigned step = gridDim.x * DO_THREADS, cols = (unsigned)a.cols;
+  unsigned u = blockIdx.x * DO_THREADS + threadIdx.x;
+  const unsigned long long at0 = (unsigned long long)u * 16, by = (unsigned long long)step * 16;
+  unsigned r = (unsigned)(at0 / cols), c = (unsigned)(at0 - (unsigned long long)r * cols);
+  const unsigned by_r = (unsigned)(by / cols), by_c = (unsigned)(by - (unsigned long long)by_r * cols);
+  const ShPhiloxKey key = sh_philox_key(seed);
+  ShRaw<T, 16> x, res;
+  auto fetch = [&](unsigned p) {
+    if (p >= a.units) return;
+    const T* px = (const T*)a.x + (long long)p * 16;
+    const T* pr = RES ? (const T*)a.residual + (long long)p * 16 : nullptr;
+    if ((long long)p * 16 + 16 <= a.values) {
+      x.load(px);
+      if constexpr (RES) res.load(pr);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const bool there = (long long)p * 16 + i < a.values;
+        reinterpret_cast<T*>(x.w)[i] = there ? px[i] : T(0.f);
+        if constexpr (RES) reinterpret_cast<T*>(res.w)[i] = there ? pr[i] : T(0.f);
+      }
+    }
+  };
+  fetch(u);
+  while (u < a.units) {
+    float f[16], add[16];
+    x.get(f);
+    if constexpr (RES) res.get(add);
+    fetch(u + step);
+    unsigned w[12], bits[8];
+    const unsigned blk = c / 8, s = c % 8;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) sh_dropout_bits(key, offset, r, blk + i, w + 4 * i);
+#pragma unroll
+    for (int i = 0; i < 10; ++i) w[i] = s & 4 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 9; ++i) w[i] = s & 2 ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) bits[i] = __funnelshift_r(w[i], w[i + 1], s & 1 ? 16 : 0);
+    const unsigned left = cols - c;                      // of the row
+    if (left < 16) {
+      unsigned v[8];
+      sh_dropout_bits(key, offset, r + 1, 0, v);
+      sh_dropout_bits(key, offset, r + 1, 1, v + 4);
+#pragma unroll
+      for (int k = 8; k >= 2; k >>= 1)                   // up by `left` halves
+#pragma unroll
+        for (int i = 7; i >= 0; --i) v[i] = left & k ? (i >= k / 2 ? v[i - k / 2] : 0u) : v[i];
+#pragma unroll
+      for (int i = 7; i >= 0; --i) v[i] = __funnelshift_l(i ? v[i - 1] : 0u, v[i], left & 1 ? 16 : 0);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const unsigned m = (2u * i < left ? 0xFFFFu : 0u) | (2u * i + 1 < left ? 0xFFFF0000u : 0u);
+        bits[i] = (bits[i] & m) | (v[i] & ~m);
+      }
+    }
+    sh_dropout_values<RES, 16>(a, bits, f, add);
+    T* y = (T*)a.y + (long long)u * 16;
+    if ((long long)u * 16 + 16 <= a.values) sh_store<T, 16>(y, f);
+    else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) if ((long long)u * 16 + i < a.values) y[i] = sh_from_float<T>(f[i]);
+    }
+    u += step; r += by_r; c += by_c;
+    if (c >= cols) { c -= cols; ++r; }
+  }
+}
+
+// What is left (rows apart and at no vector's address, or very short): lanes that took 8 neighbouring values each would touch every 32-byte sector eight
+// times over, so a group of lanes (4 to 32, 8 columns each) reads and writes its segment of a row one value a lane, one behind
+// the other, and its pieces go through shared memory.  16384 x 2001 in bf16: 73 us; with each lane's values straight from memory 91.
+template <typename T, bool RES>
+static __global__ void __launch_bounds__(DO_THREADS) sh_dropout_rows_kernel(const DoArgs a) {
+  constexpr int N = 8, ACC = 1;
+  __shared__ __align__(16) T s_x[DO_THREADS / 32][256], s_r[RES ? DO_THREADS / 32 : 1][256];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const unsigned long long seed = __ldg(a.rng), offset = __ldg(a.rng + 1);
+  const ShPhiloxKey key = sh_philox_key(seed);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, G = 1 << a.group_log, g = lane >> a.group_log, j = lane & (G - 1);
+  const unsigned step = gridDim.x * (DO_THREADS >> a.group_log);
+  T* sx = s_x[warp] + g * 8 * G;                         // the group's segment
+  T* sr = RES ? s_r[warp] + g * 8 * G : nullptr;
+  // (a warp's groups go round together)
+  const unsigned first = (blockIdx.x * (DO_THREADS / 32) + warp) << (5 - a.group_log);
+  ShRaw<T, ACC> x[N], res[N];
+  auto fetch = [&](unsigned u) {
+    const unsigned r = u / a.segs, c0 = (u - r * a.segs) * 8 * G;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const unsigned c = c0 + (i * G + j) * ACC;
+      if (u < a.groups && c < (unsigned)a.cols) {
+        x[i].load((const T*)a.x + (long long)r * a.xs + c);
+        if constexpr (RES) res[i].load((const T*)a.residual + (long long)r * a.rs + c);
+      } else {
+        x[i].fill(0);
+        if constexpr (RES) res[i].fill(0);
+      }
+    }
+  };
+  fetch(first + g);
+  for (unsigned w = first; w < a.groups; w += step) {
+    const unsigned u = w + g, r = u / a.segs, seg = u - r * a.segs, blk = seg * G + j;
+    float f[8], add[8];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      x[i].put(sx + (i * G + j) * ACC);
+      if constexpr (RES) res[i].put(sr + (i * G + j) * ACC);
+    }
+    __syncwarp();
+    ShRaw<T, 8> piece;
+    piece.take((const unsigned char*)(sx + j * 8));
+    piece.get(f);
+    if constexpr (RES) { piece.take((const unsigned char*)(sr + j * 8)); piece.get(add); }
+    fetch(u + step);
+    sh_dropout_piece<RES>(a, key, offset, r, blk, f, add);
+    sh_store<T, 8>(sx + j * 8, f);                       // (its own piece, which nobody else reads)
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const unsigned c = seg * 8 * G + (i * G + j) * ACC;
+      ShRaw<T, ACC> out;
+      out.take((const unsigned char*)(sx + (i * G + j) * ACC));
+      if (u < a.groups && c < (unsigned)a.cols) out.put((T*)a.y + (long long)r * a.ys + c);
+    }
+    __syncwarp();
   }
 }

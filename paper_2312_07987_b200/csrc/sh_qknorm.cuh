@@ -16,9 +16,10 @@ constexpr int QN_THREADS = 256;
 
 constexpr int QN_MAX_D = 256;
 // The backward kernel's vectors are of 4 values at most (8 of a 16-bit type: 128 registers and spills; 33.5 M values of 16384 tokens, 16 heads
-// of 128: 56 us, with 4 44), and its blocks 3 to an SM (fp32, whose rows on their way are twice as large: 2; 8 x 256 tokens: 13.5 us with 3, 9.0).
+// of 128: 56 us, with 4 44), and its blocks 3 to an SM (fp32, whose rows on their way are twice as large, and vectors of one value: 2; 8 x 256
+// tokens in fp32: 13.5 us with 3, 9.0).
 constexpr int QN_BACKWARD_V = 4;
-template <typename T> __host__ __device__ constexpr int qn_backward_blocks() { return sizeof(T) == 4 ? 2 : 3; }
+template <typename T, int V> __host__ __device__ constexpr int qn_backward_blocks() { return sizeof(T) == 4 || V == 1 ? 2 : 3; }
 constexpr int QN_MAX_BLOCKS = 1024;       // blocks of the backward kernel at most (rows of its partial gain gradients)
 
 struct QnSide {
@@ -227,7 +228,7 @@ static __global__ void __launch_bounds__(QN_THREADS, 3) sh_qk_norm_kernel(const 
 // A thread adds its columns' share of the gain gradients over its rows; the block's groups are added in order in shared
 // memory, the blocks by sh_qk_norm_gain_kernel: the same bits on every run.
 template <typename T, int V, int NV, int LANES, bool PAIRED>
-static __global__ void __launch_bounds__(QN_THREADS, qn_backward_blocks<T>()) sh_qk_norm_backward_kernel(const __grid_constant__ QnArgs a) {
+static __global__ void __launch_bounds__(QN_THREADS, qn_backward_blocks<T, V>()) sh_qk_norm_backward_kernel(const __grid_constant__ QnArgs a) {
   __shared__ unsigned long long s_freq[QN_MAX_D / 2];
   extern __shared__ float s_sum[];                       // [groups][D]
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

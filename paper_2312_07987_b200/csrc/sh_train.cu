@@ -168,7 +168,7 @@ int qn_run(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, bool 
   if (backward) {
     long long n[2];
     for (int i = 0; i < 2; ++i) n[i] = (items[i] + groups - 1) / groups;
-    const long long fit = (long long)sms * (p.dtype == SH_F32 ? qn_backward_blocks<float>() : qn_backward_blocks<__half>()), cap = fit < QN_MAX_BLOCKS ? fit : QN_MAX_BLOCKS;
+    const long long fit = (long long)sms * (p.dtype == SH_F32 ? qn_backward_blocks<float, 4>() : v == 1 ? qn_backward_blocks<__half, 1>() : qn_backward_blocks<__half, 4>()), cap = fit < QN_MAX_BLOCKS ? fit : QN_MAX_BLOCKS;
     if (n[0] + n[1] > cap) {                               // shares by the sides' rows
       const long long all = n[0] + n[1];
       const long long b0 = n[0] ? (n[0] * cap + all / 2) / all : 0;
@@ -381,28 +381,40 @@ int sh_run_dropout(const sh_dropout_args& p, bool pdl, cudaStream_t st) {
   const size_t size = elem_bytes(p.dtype);
   auto aligned = [&](const void* q, long long stride) { return (uintptr_t)q % 16 == 0 && (p.rows == 1 || (size_t)stride * size % 16 == 0); };
   const bool vec = aligned(p.x, p.x_stride) && aligned(p.y, p.y_stride) && (!p.residual || aligned(p.residual, p.residual_stride));
-  const bool dense = vec && p.cols % 8 == 0 && p.x_stride == p.cols && p.y_stride == p.cols && (!p.residual || p.residual_stride == p.cols);
+  const bool whole = p.rows == 1 || (p.x_stride == p.cols && p.y_stride == p.cols && (!p.residual || p.residual_stride == p.cols));   // one run of values
+  const bool dense = vec && whole && p.cols % 8 == 0;
+  const bool base = (((uintptr_t)p.x | (uintptr_t)p.y | (uintptr_t)p.residual) & 15) == 0;
+  const bool flat = !vec && whole && base && p.cols >= 16 && p.rows < (1ll << 34) / p.cols;
   DoArgs a;
   a.rng = (const unsigned long long*)p.rng;
   a.xs = p.x_stride; a.rs = p.residual_stride; a.ys = p.y_stride;
   a.cols = (int)p.cols;
   a.upr = (unsigned)((p.cols + 7) / 8);
+  a.group_log = 2;
+  while (a.group_log < 5 && (1u << a.group_log) < a.upr) ++a.group_log;
+  a.segs = (unsigned)((a.upr + (1u << a.group_log) - 1) >> a.group_log);
   const int limit = (int)lrint(p.p * 65536.0);
   a.none = limit > 65535; a.limit = a.none ? 0u : (unsigned)limit << 16;
   a.scale = a.none ? 0.f : (float)(65536.0 / (65536 - limit));
-  const long long most = (1ll << 31) / a.upr < 1 ? 1 : (1ll << 31) / a.upr;           // rows of a launch
+  const long long most = flat ? p.rows : (1ll << 31) / a.upr < 1 ? 1 : (1ll << 31) / a.upr;           // rows of a launch
   for (long long r = 0; r < p.rows; r += most) {
     const long long n = p.rows - r < most ? p.rows - r : most;
     a.x = (const char*)p.x + r * p.x_stride * (long long)size; a.y = (char*)p.y + r * p.y_stride * (long long)size;
     a.residual = p.residual ? (const char*)p.residual + r * p.residual_stride * (long long)size : nullptr;
     a.row0 = (unsigned)r; a.units = (unsigned)(n * a.upr);
-    const long long blocks = ((long long)a.units + DO_THREADS - 1) / DO_THREADS, cap = 8ll * sms;
+    a.groups = (unsigned)(n * a.segs);
+    a.values = n * p.cols;
+    if (flat) a.units = (unsigned)((a.values + 15) / 16);
+    const long long threads = vec || flat ? a.units : (long long)a.groups << a.group_log;
+    const long long blocks = (threads + DO_THREADS - 1) / DO_THREADS, cap = 8ll * sms;
     const dim3 grid((unsigned)(blocks < cap ? blocks : cap));
     auto go = [&](auto kern) { return launch_k(pdl, kern, grid, dim3(DO_THREADS), 0, st, a); };
     auto typed = [&](auto zero) {
       using T = decltype(zero);
-      if (p.residual) return dense ? go(sh_dropout_kernel<T, DO_DENSE, true>) : vec ? go(sh_dropout_kernel<T, DO_VECTORS, true>) : go(sh_dropout_kernel<T, DO_VALUES, true>);
-      return dense ? go(sh_dropout_kernel<T, DO_DENSE, false>) : vec ? go(sh_dropout_kernel<T, DO_VECTORS, false>) : go(sh_dropout_kernel<T, DO_VALUES, false>);
+      if (p.residual) return dense ? go(sh_dropout_kernel<T, DO_DENSE, true>) : vec ? go(sh_dropout_kernel<T, DO_VECTORS, true>)
+                           : flat ? go(sh_dropout_flat_kernel<T, true>) : go(sh_dropout_rows_kernel<T, true>);
+      return dense ? go(sh_dropout_kernel<T, DO_DENSE, false>) : vec ? go(sh_dropout_kernel<T, DO_VECTORS, false>)
+           : flat ? go(sh_dropout_flat_kernel<T, false>) : go(sh_dropout_rows_kernel<T, false>);
     };
     const int rc = p.dtype == SH_F32 ? typed(0.f) : p.dtype == SH_BF16 ? typed(__nv_bfloat16()) : typed(__half());
     if (rc) return rc;
