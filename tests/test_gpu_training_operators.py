@@ -58,9 +58,10 @@ def norm_bounds(x, gain, eps, scale):
 
 # the sum of squares: at most 16 additions in a lane, 5 across lanes, so 21 U, of which the root keeps half; rsqrtf 4 U; gain, scale, r: 4 U
 NORM_U = 20
-# sine and cosine: the angle is off by 2^-25 turns (its upper 32 bits as a float: half a step of 2^-24 of a half turn) = 2 pi 2^-25 = 3.2 U,
-# sincospif by 2 U; two products and a sum: 3 U
-TURN_U = 9
+# sine and cosine: the angle is off by 2^-26 turns (its upper 32 bits as a float: half a step of 2^-24 of a half turn) = 2 pi 2^-26 = 1.6 U; fp32:
+# sincospif by 2 U; 16-bit types: sin.approx and cos.approx by 2^-20.9 (the instruction's documented bound) = 8.6 U and their argument, the
+# rounded product of pi, by 1.6 U more; two products and a sum: 3 U
+TURN_U = 15
 
 CASES = [  # B, T, Hq, Hk, D, rotated, halves, layout, dtype, q_scale
     (2, 5, 4, 4, 128, 128, False, "fused", "bf16", 1.0),
@@ -277,6 +278,33 @@ def test_balance_many_tokens(kind):
 
 
 @pytest.mark.parametrize("kind", ["counts", "entropy"])
+@pytest.mark.parametrize("N,S,H,E,ty", [(40000, 1, 2, 4, "f32"), (9001, 2, 2, 16, "f32"), (9001, 1, 2, 31, "f32"), (70001, 1, 1, 3, "bf16"), (20003, 1, 2, 8, "bf16"), (9000, 1, 3, 16, "bf16"),
+                                        (9001, 1, 1, 32, "bf16"), (9001, 1, 2, 20, "bf16"), (30, 2, 600, 8, "f32"), (3, 2, 40, 32, "bf16")])
+def test_balance_of_two_launches(N, S, H, E, ty, kind):
+    """Above the sizes of the kernel of one launch, every width of a row: against fp64 sums."""
+    z, idx, mask = balance_inputs(N, S, H, E, min(3, E - 1), TYPES[ty], True)
+    got = b.sh_balance_loss(z, idx, kind=kind, coef=0.1, mask=mask)
+    dz = b.sh_balance_backward(z, got["slope"], mask=mask)
+    n = int(mask.sum())
+    p = torch.softmax(z.double(), -1) * mask[:, None, None, None]
+    P = p.sum(0) / n
+    picks = (idx.long()[..., None] == torch.arange(E, device="cuda")) & mask[None, :, None, None, None]
+    counts = picks.sum((1, 3))
+    assert torch.equal(got["counts"].long(), counts)
+    f = counts.double() / counts.sum(-1, keepdim=True)
+    c = 0.1 * E * f if kind == "counts" else 0.1 * torch.log(P)
+    loss = (0.1 * E * (f * P).sum() if kind == "counts" else 0.1 * (P * torch.log(P)).sum()).item()
+    want = p * (c - (p * c).sum(-1, keepdim=True)) / n
+    # (p: 40 U, as above with logits of up to 8 and their differences; P: and a thread's additions, N / 444 rows at most, a block's 256)
+    p_u = (18 + 2 * float(z.float().abs().max())) * U
+    P_u = p_u + (N / 444 + 256 + 2) * U
+    close(got["prob"], host(P), host(P) * P_u, torch.float32)
+    log = float(torch.log(P).abs().max())
+    close(got["loss"], loss, 0.1 * S * H * (E if kind == "counts" else 1 + log) * P_u, torch.float32)
+    close(dz, host(want), host(p) * 0.1 * (2 * (E if kind == "counts" else 1 + log) * (p_u + 16 * U) + 2 * P_u) / n, TYPES[ty])
+
+
+@pytest.mark.parametrize("kind", ["counts", "entropy"])
 def test_balance_extreme_logits(kind):
     z, idx, mask = balance_inputs(64, 2, 2, 8, 2, torch.float32, False)
     z[:, 0, 0, 3] = -float("inf")                          # an expert that is switched off for everyone
@@ -347,6 +375,43 @@ def test_dropout(rows, cols, ty, residual):
         want = np.where(kept, host(x) * scale, 0.0) + r
         close(y, want, 3 * U * (np.abs(host(x)) * scale + np.abs(r)), t)      # (the factor, the product, the sum)
         assert np.array_equal(host(y)[~kept], r[~kept])                       # what is dropped leaves the residual's bits
+
+
+@pytest.mark.parametrize("ty", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,cols", [(64, 17), (41, 23), (7, 1001), (300, 31), (9, 18), (5, 20), (1, 33), (2, 4095), (700, 19)])
+def test_dropout_dense_rows_of_any_length(rows, cols, ty):
+    # a thread's 16 values begin anywhere in a piece, end in the next row, and at the end of the matrix
+    t = TYPES[ty]
+    x, res = torch.randn(rows, cols, device="cuda").to(t), torch.randn(rows, cols, device="cuda").to(t)
+    rng = torch.tensor([cols, 1 << 33], device="cuda")
+    kept, scale = op.dropout_kept(rows, cols, cols, 1 << 33, 0.4)
+    for r in (None, res):
+        add = np.zeros((rows, cols)) if r is None else host(r)
+        y = b.sh_dropout(x, rng, 0.4, residual=r)
+        close(y, np.where(kept, host(x) * scale, 0.0) + add, 3 * U * (np.abs(host(x)) * scale + np.abs(add)), t)
+        assert np.array_equal(host(y)[~kept], add[~kept])
+    whole = torch.full((rows * cols + 32,), 9.0, device="cuda", dtype=t)                # what lies behind the last value stays
+    out = whole[:rows * cols].view(rows, cols)
+    assert torch.equal(b.sh_dropout(x, rng, 0.4, out=out), b.sh_dropout(x, rng, 0.4)) and (whole[rows * cols:] == 9).all()
+
+
+@pytest.mark.parametrize("ty", ["f32", "bf16"])
+@pytest.mark.parametrize("stride,cols", [(80, 77), (79, 77), (88, 80), (83, 40), (24, 9), (11, 5), (2008, 2001), (2003, 2001), (640, 513)])
+def test_dropout_rows_apart(stride, cols, ty):
+    # rows at vectors' addresses that end inside a piece, and rows anywhere: the same values as a dense matrix's
+    t, rows = TYPES[ty], 37
+    x, res = torch.randn(rows, cols, device="cuda").to(t), torch.randn(rows, cols, device="cuda").to(t)
+    rng = torch.tensor([1, 2], device="cuda")
+    want, plain = b.sh_dropout(x, rng, 0.3, residual=res), b.sh_dropout(x, rng, 0.3)
+    wide = torch.full((rows, stride), 5.0, device="cuda", dtype=t)
+    view = wide[:, :cols]
+    view.copy_(x)
+    assert torch.equal(b.sh_dropout(view, rng, 0.3), plain)
+    assert b.sh_dropout(view, rng, 0.3, residual=res, out=view) is view
+    assert torch.equal(view, want) and (wide[:, cols:] == 5).all()
+    off = torch.empty(rows * cols + 1, device="cuda", dtype=t)[1:].view(rows, cols)         # dense, one value off alignment
+    off.copy_(x)
+    assert torch.equal(b.sh_dropout(off, rng, 0.3), plain)
 
 
 def test_dropout_shapes_strides_and_places():
