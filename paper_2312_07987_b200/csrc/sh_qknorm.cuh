@@ -15,26 +15,40 @@
 constexpr int QN_THREADS = 256;
 
 constexpr int QN_MAX_D = 256;
+constexpr int QN_PAIRS = QN_MAX_D / 2;    // (as many as the widest row's lanes hold)
 // The backward kernel's vectors are of 4 values at most (8 of a 16-bit type: 128 registers and spills; 33.5 M values of 16384 tokens, 16 heads
-// of 128: 56 us, with 4 44), and its blocks 3 to an SM (fp32, whose rows on their way are twice as large, and vectors of one value: 2; 8 x 256
+// of 128: 56 us, with 4 44), and its blocks 3 to an SM (fp32, whose rows on their way are twice as large, vectors of one value, and six of two: 2; 8 x 256
 // tokens in fp32: 13.5 us with 3, 9.0).
 constexpr int QN_BACKWARD_V = 4;
-template <typename T, int V> __host__ __device__ constexpr int qn_backward_blocks() { return sizeof(T) == 4 || V == 1 ? 2 : 3; }
+template <typename T, int V, int NV> __host__ __device__ constexpr int qn_backward_blocks() { return sizeof(T) == 4 || V == 1 || NV == 6 ? 2 : 3; }
 constexpr int QN_MAX_BLOCKS = 1024;       // blocks of the backward kernel at most (rows of its partial gain gradients)
+
+// Division of 0 <= n < 2^31 by d >= 1 (0: nothing is divided): (n + upper half of n m) >> s.
+struct QnDiv { unsigned d, m, s; };
+inline QnDiv qn_divisor(unsigned d) {
+  QnDiv r{d, 0, 0};
+  if (d == 0) return r;
+  while ((1ull << r.s) < d) ++r.s;
+  r.m = (unsigned)(((1ull << 32) * ((1ull << r.s) - d)) / d + 1);
+  return r;
+}
 
 struct QnSide {
   const void* x; const void* dy; void* out;              // out: y, or dx
   const float* gain;
   float* dgain;                                          // nullptr: not wanted
   long long xb, xt, xh, yb, yt, yh, ob, ot, oh;          // strides of batch, token, head (elements): of x, dy, out
-  int heads, chunks;                                     // chunks of up to `per` heads
+  int heads;
+  QnDiv chunks;                                          // chunks of up to `per` heads
   float scale;
 };
 struct QnArgs {
   QnSide s[2];
   const void* pos;                                       // [batch, seq] or nullptr: the token's place in its sequence
   int pos64, next;                                       // next: rotated pairs are neighbouring columns
-  int seq, D, R;                                         // R: rotated columns
+  QnDiv seq, chunks;                                     // chunks: of both sides
+  int large;                                             // (token, chunk) numbers of 2^31 and more
+  int D, R;                                              // R: rotated columns
   int per;                                               // heads to a group
   long long tokens;                                      // batch * seq
   int blocks0;                                           // backward: blocks of the queries (the rest: keys)
@@ -124,47 +138,49 @@ __device__ __forceinline__ void qn_gains(const float* gain, const int (&col)[NV]
   qn_get<float, V, NV, PAIRED>(raw, g);
 }
 
-// cos and sin of pair n at a position: 1 and 0 behind the rotated columns.  16-bit results: the special function unit's (off by
-// 2^-21, where a result's half step is 2^-12 at least); fp32: sincospif.
-template <typename T, int V, int NV, bool PAIRED>
-__device__ __forceinline__ void qn_angle(const QnArgs& a, const unsigned long long* freq, long long pos, const int (&col)[NV], int n, float* cs, float* sn) {
-  const int c = col[qn_vec_a<V, PAIRED>(n)], at = c + qn_at_a<V, PAIRED>(n);
-  const bool next = !PAIRED || (V == 1 && a.next);
-  const int pair = next ? at / 2 : at;
-  *cs = 1.f; *sn = 0.f;
-  if (c >= 0 && pair < a.R / 2) {
-    const unsigned long long f = freq[pair];
-    // (the upper half of the product's lower 64 bits: half turns times 2^31)
-    const float x = (float)(int)(__umulhi((unsigned)pos, (unsigned)f) + (unsigned)pos * (unsigned)(f >> 32) + (unsigned)(pos >> 32) * (unsigned)f);
-    if constexpr (sizeof(T) == 2) __sincosf(x * (3.14159265f * 4.656612873077393e-10f), sn, cs);
-    else sincospif(x * 4.656612873077393e-10f, sn, cs);
-  }
+// The frequencies into shared memory; zeros behind the rotated columns, whose cos and sin are then 1 and 0 without a branch.
+__device__ __forceinline__ void qn_frequencies(const QnArgs& a, unsigned long long* freq) {
+  for (int i = threadIdx.x; i < QN_PAIRS; i += QN_THREADS) freq[i] = i < a.R / 2 ? a.freq[i] : 0ull;
+}
+
+// cos and sin of the lane's pair n at a position.  16-bit results: the special function unit's (off by 2^-21, where a result's half
+// step is 2^-12 at least); fp32: sincospif.
+template <typename T, int V, int NV, int LANES, bool PAIRED>
+__device__ __forceinline__ void qn_angle(const unsigned long long* freq, int l, long long pos, int n, float* cs, float* sn) {
+  // (pairs in the order of the lanes' columns: neighbours by their first column, halves by the first one's)
+  const int pair = PAIRED ? (l + n / V * LANES) * V + n % V : ((l + 2 * n / V * LANES) * V + 2 * n % V) / 2;
+  const unsigned long long f = freq[pair];
+  // (the upper half of the product's lower 64 bits: half turns times 2^31)
+  const float x = (float)(int)(__umulhi((unsigned)pos, (unsigned)f) + (unsigned)pos * (unsigned)(f >> 32) + (unsigned)(pos >> 32) * (unsigned)f);
+  if constexpr (sizeof(T) == 2) __sincosf(x * (3.14159265f * 4.656612873077393e-10f), sn, cs);
+  else sincospif(x * 4.656612873077393e-10f, sn, cs);
 }
 
 __device__ __forceinline__ long long qn_position(const QnArgs& a, long long token, int t) {
   if (!a.pos) return t;
   return a.pos64 ? __ldg((const long long*)a.pos + token) : (long long)__ldg((const int*)a.pos + token);
 }
-__device__ __forceinline__ long long qn_div(long long n, int d) { return n >> 32 ? n / d : (long long)((unsigned)n / (unsigned)d); }
+__device__ __forceinline__ long long qn_div(const QnArgs& a, long long n, const QnDiv& d) {
+  return a.large ? n / d.d : (long long)((__umulhi((unsigned)n, d.m) + (unsigned)n) >> d.s);
+}
 
 // V = 1 without pairs: nothing is rotated (d_head may be odd).
 template <typename T, int V, int NV, int LANES, bool PAIRED>
 static __global__ void __launch_bounds__(QN_THREADS, 3) sh_qk_norm_kernel(const __grid_constant__ QnArgs a) {
-  __shared__ unsigned long long s_freq[QN_MAX_D / 2];
+  __shared__ __align__(16) unsigned long long s_freq[QN_PAIRS];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   constexpr int P = NV * V / 2;
-  for (int i = threadIdx.x; i < a.R / 2; i += QN_THREADS) s_freq[i] = a.freq[i];
+  if (a.R) qn_frequencies(a, s_freq);
   const int l = threadIdx.x % LANES;
   const long long item = (long long)blockIdx.x * (QN_THREADS / LANES) + threadIdx.x / LANES;
-  const int chunks = a.s[0].chunks + a.s[1].chunks;
-  const long long token = qn_div(item, chunks);
+  const long long token = qn_div(a, item, a.chunks);
   const bool live = token < a.tokens;                    // (a warp's groups shuffle together: none leaves early)
-  int chunk = (int)(item - token * chunks);
-  const int side = chunk >= a.s[0].chunks;
+  int chunk = (int)(item - token * a.chunks.d);
+  const int side = chunk >= (int)a.s[0].chunks.d;
   const QnSide& s = a.s[side];
-  if (side) chunk -= a.s[0].chunks;
-  const long long b = qn_div(token, a.seq);
-  const int t = (int)(token - b * a.seq);
+  if (side) chunk -= a.s[0].chunks.d;
+  const long long b = qn_div(a, token, a.seq);
+  const int t = (int)(token - b * a.seq.d);
   const int h0 = chunk * a.per, n = live ? min(a.per, s.heads - h0) : 0;
   int col[NV];
   qn_columns<V, NV, LANES, PAIRED>(a, l, col);
@@ -194,7 +210,7 @@ static __global__ void __launch_bounds__(QN_THREADS, 3) sh_qk_norm_kernel(const 
   for (int m = 0; m < P; ++m) {
     float cs = 1.f, sn = 0.f;
     if constexpr (V > 1 || PAIRED)
-      if (a.R) qn_angle<T, V, NV, PAIRED>(a, s_freq, pos, col, m, &cs, &sn);
+      if (a.R) qn_angle<T, V, NV, LANES, PAIRED>(s_freq, l, pos, m, &cs, &sn);
     const float ga = s.scale * qn_half(g.a[m / 2], m & 1), gb = s.scale * qn_half(g.b[m / 2], m & 1);
     qn_half(fa.a[m / 2], m & 1) = ga * cs; qn_half(fa.b[m / 2], m & 1) = -gb * sn;
     qn_half(fb.a[m / 2], m & 1) = ga * sn; qn_half(fb.b[m / 2], m & 1) = gb * cs;
@@ -228,13 +244,13 @@ static __global__ void __launch_bounds__(QN_THREADS, 3) sh_qk_norm_kernel(const 
 // A thread adds its columns' share of the gain gradients over its rows; the block's groups are added in order in shared
 // memory, the blocks by sh_qk_norm_gain_kernel: the same bits on every run.
 template <typename T, int V, int NV, int LANES, bool PAIRED>
-static __global__ void __launch_bounds__(QN_THREADS, qn_backward_blocks<T, V>()) sh_qk_norm_backward_kernel(const __grid_constant__ QnArgs a) {
-  __shared__ unsigned long long s_freq[QN_MAX_D / 2];
+static __global__ void __launch_bounds__(QN_THREADS, qn_backward_blocks<T, V, NV>()) sh_qk_norm_backward_kernel(const __grid_constant__ QnArgs a) {
+  __shared__ __align__(16) unsigned long long s_freq[QN_PAIRS];
   extern __shared__ float s_sum[];                       // [groups][D]
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   constexpr int P = NV * V / 2, GROUPS = QN_THREADS / LANES;
-  for (int i = threadIdx.x; i < a.R / 2; i += QN_THREADS) s_freq[i] = a.freq[i];
+  if (a.R) qn_frequencies(a, s_freq);
   if (a.R) __syncthreads();
   const int l = threadIdx.x % LANES, group = threadIdx.x / LANES;
   const int side = (int)blockIdx.x >= a.blocks0;
@@ -247,15 +263,15 @@ static __global__ void __launch_bounds__(QN_THREADS, qn_backward_blocks<T, V>())
 #pragma unroll
   for (int m = 0; m < P / 2; ++m) dg.a[m] = dg.b[m] = make_float2(0.f, 0.f);
   const float inv = 1.f / (float)a.D;
-  const long long items = a.tokens * s.chunks, step = (long long)blocks * GROUPS;
+  const long long items = a.tokens * s.chunks.d, step = (long long)blocks * GROUPS;
   // (rounds: the same for every group of the block)
   for (long long first = (long long)block * GROUPS; first < items; first += step) {
     const long long item = first + group;
     const bool live = item < items;
-    const long long token = live ? qn_div(item, s.chunks) : 0;
-    const int h0 = live ? (int)(item - token * s.chunks) * a.per : 0, n = live ? min(a.per, s.heads - h0) : 0;
-    const long long b = qn_div(token, a.seq);
-    const int t = (int)(token - b * a.seq);
+    const long long token = live ? qn_div(a, item, s.chunks) : 0;
+    const int h0 = live ? (int)(item - token * s.chunks.d) * a.per : 0, n = live ? min(a.per, s.heads - h0) : 0;
+    const long long b = qn_div(a, token, a.seq);
+    const int t = (int)(token - b * a.seq.d);
     const T* px = (const T*)s.x + b * s.xb + t * s.xt + h0 * s.xh + col[0];
     const T* pd = (const T*)s.dy + b * s.yb + t * s.yt + h0 * s.yh + col[0];
     T* po = (T*)s.out + b * s.ob + t * s.ot + h0 * s.oh + col[0];
@@ -281,7 +297,7 @@ static __global__ void __launch_bounds__(QN_THREADS, qn_backward_blocks<T, V>())
     for (int m = 0; m < P; ++m) {
       float c = 1.f, d = 0.f;
       if constexpr (V > 1 || PAIRED)
-        if (a.R) qn_angle<T, V, NV, PAIRED>(a, s_freq, pos, col, m, &c, &d);
+        if (a.R) qn_angle<T, V, NV, LANES, PAIRED>(s_freq, l, pos, m, &c, &d);
       qn_half(cs[m / 2], m & 1) = s.scale * c; qn_half(sn[m / 2], m & 1) = s.scale * d;
     }
     for (int j0 = 0; j0 < a.per; j0 += 2) {
@@ -306,7 +322,8 @@ static __global__ void __launch_bounds__(QN_THREADS, qn_backward_blocks<T, V>())
           u.a[m] = __fmul2_rn(u.a[m], g.a[m]);
           u.b[m] = __fmul2_rn(u.b[m], g.b[m]);
         }
-        const float sum = sh_group_sum<LANES>(ss.x + ss.y), dot = sh_group_sum<LANES>(wx.x + wx.y);
+        float sum = ss.x + ss.y, dot = wx.x + wx.y;
+        sh_group_sums<LANES>(sum, dot);
         float r = rsqrtf(fmaf(sum, inv, a.eps));
         if (j0 + q >= n) r = 0.f;                        // (no row: what is left of the last one does not count)
         const float rm = -(dot * inv * r * r) * r;

@@ -102,7 +102,7 @@ void qn_fill(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, QnA
   side(a.s[1], p.k, p.k_out, back ? back->dk : none, p.gk, back ? back->dgk : nullptr, p.k_heads, 1.f);
   a.pos = p.positions; a.pos64 = p.positions_64 != 0;
   a.next = p.rotated && !p.halves;
-  a.seq = p.seq; a.D = p.d_head; a.R = p.rotated;
+  a.seq = qn_divisor((unsigned)p.seq); a.D = p.d_head; a.R = p.rotated;
   a.tokens = (long long)p.batch * p.seq;
   a.eps = p.eps;
   a.blocks0 = 0; a.part = nullptr;
@@ -115,15 +115,18 @@ void qn_fill(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, QnA
 }
 
 constexpr int qn_vectors(int v) { return v >= 4 ? 2 : v == 2 ? 4 : 8; }
-// Lanes to a row: 4 to 32 (vectors of two values, where half the rotated width is odd, or less: 16 or 32).
+// Vectors of two values and d_head 129 to 192: six to a lane, 16 lanes, where 32 with four each leave a third or more of them idle.
+constexpr int QN_SIX = 6;
+bool qn_six(int v, int d_head) { return v == 2 && d_head > 128 && d_head <= 192; }
+// Lanes to a row: 4 to 32 (vectors of two values, where a quarter of the rotated width is odd, or less: 16 or 32).
 int qn_lanes(int v, int d_head) {
+  if (qn_six(v, d_head)) return 16;
   const int n = pow2_at_least((d_head + v * qn_vectors(v) - 1) / (v * qn_vectors(v))), least = v == 8 ? 4 : v == 4 ? 8 : 16;
   return n > least ? n : least;
 }
 
-template <typename T, int V, int LANES, bool PAIRED>
+template <typename T, int V, int LANES, bool PAIRED, int NV = qn_vectors(V)>
 int qn_launch(const QnArgs& a, bool backward, bool pdl, int blocks, cudaStream_t st) {
-  constexpr int NV = qn_vectors(V);
   if (!backward) return launch_k(pdl, sh_qk_norm_kernel<T, V, NV, LANES, PAIRED>, dim3((unsigned)blocks), dim3(QN_THREADS), 0, st, a);
   const size_t sums = (size_t)(QN_THREADS / LANES) * a.D * 4;
   if constexpr (V <= QN_BACKWARD_V) return launch_k(pdl, sh_qk_norm_backward_kernel<T, V, NV, LANES, PAIRED>, dim3((unsigned)blocks), dim3(QN_THREADS), sums, st, a);
@@ -133,6 +136,8 @@ int qn_launch(const QnArgs& a, bool backward, bool pdl, int blocks, cudaStream_t
 template <typename T, int V, bool PAIRED>
 int qn_lanes_of(const QnArgs& a, int lanes, bool backward, bool pdl, int blocks, cudaStream_t st) {
   constexpr int LEAST = V == 8 ? 4 : V == 4 ? 8 : 16;
+  if constexpr (V == 2)
+    if (qn_six(V, a.D)) return qn_launch<T, V, 16, PAIRED, QN_SIX>(a, backward, pdl, blocks, st);
   if (lanes == LEAST) return qn_launch<T, V, LEAST, PAIRED>(a, backward, pdl, blocks, st);
   if constexpr (LEAST < 16)
     if (lanes == 2 * LEAST) return qn_launch<T, V, 2 * LEAST, PAIRED>(a, backward, pdl, blocks, st);
@@ -162,13 +167,16 @@ int qn_run(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, bool 
   a.per = most < 8 ? (most < 1 ? 1 : most) : 8;
   auto chunks = [&](int i) { return (a.s[i].heads + a.per - 1) / a.per; };
   while (a.per > 1 && a.tokens * (chunks(0) + chunks(1)) < 4ll * sms * groups) a.per = a.per > 2 ? (a.per + 1) / 2 : 1;
-  a.s[0].chunks = chunks(0); a.s[1].chunks = chunks(1);
-  const long long items[2] = {a.tokens * a.s[0].chunks, a.tokens * a.s[1].chunks};
+  const int c[2] = {chunks(0), chunks(1)};
+  const long long items[2] = {a.tokens * c[0], a.tokens * c[1]};
+  for (int i = 0; i < 2; ++i) a.s[i].chunks = qn_divisor((unsigned)c[i]);
+  a.chunks = qn_divisor((unsigned)(c[0] + c[1]));
+  a.large = items[0] + items[1] > (1ll << 31) - (1 << 24);   // (a grid's last round goes past the end)
   long long blocks = (items[0] + items[1] + groups - 1) / groups;
   if (backward) {
     long long n[2];
     for (int i = 0; i < 2; ++i) n[i] = (items[i] + groups - 1) / groups;
-    const long long fit = (long long)sms * (p.dtype == SH_F32 ? qn_backward_blocks<float, 4>() : v == 1 ? qn_backward_blocks<__half, 1>() : qn_backward_blocks<__half, 4>()), cap = fit < QN_MAX_BLOCKS ? fit : QN_MAX_BLOCKS;
+    const long long fit = (long long)sms * (p.dtype == SH_F32 ? qn_backward_blocks<float, 4, 2>() : v == 1 ? qn_backward_blocks<__half, 1, 8>() : qn_six(v, p.d_head) ? qn_backward_blocks<__half, 2, QN_SIX>() : qn_backward_blocks<__half, 4, 2>()), cap = fit < QN_MAX_BLOCKS ? fit : QN_MAX_BLOCKS;
     if (n[0] + n[1] > cap) {                               // shares by the sides' rows
       const long long all = n[0] + n[1];
       const long long b0 = n[0] ? (n[0] * cap + all / 2) / all : 0;

@@ -89,3 +89,14 @@ __device__ __forceinline__ float sh_group_sum(float v) {
   for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
+// Two of them at once: after one exchange each half of a group adds one.
+template <int LANES>
+__device__ __forceinline__ void sh_group_sums(float& a, float& b) {
+  const bool up = threadIdx.x & (LANES / 2);
+  float v = (up ? b : a) + __shfl_xor_sync(0xffffffffu, up ? a : b, LANES / 2);
+#pragma unroll
+  for (int o = LANES / 4; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  const float w = __shfl_xor_sync(0xffffffffu, v, LANES / 2);
+  a = up ? w : v;
+  b = up ? v : w;
+}
