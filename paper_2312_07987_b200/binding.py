@@ -365,34 +365,30 @@ _DTYPES = {torch.float32: SH_F32, torch.bfloat16: SH_BF16, torch.float16: SH_F16
 _NO_HEADS = (0, 0, 0, 0)
 
 
+_current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream    # (torch.cuda's own make objects first: 2 us of a 10 us call)
+
+
 def _launch(fn, packed: bytes, device: int) -> None:
     """The call on the tensors' device and on the stream that is current there."""
-    if device == torch.cuda.current_device():
-        rc = fn(packed, torch._C._cuda_getCurrentRawStream(device))     # (torch.cuda.current_stream makes an object first: 2 us of a 10 us call)
+    if device == _current_device():
+        rc = fn(packed, _raw_stream(device))
     else:
         with torch.cuda.device(device):
-            rc = fn(packed, torch._C._cuda_getCurrentRawStream(device))
+            rc = fn(packed, _raw_stream(device))
     if rc != SH_OK:
         raise SwitchHeadError(rc)
 
 
-def _strides(t: torch.Tensor) -> tuple:
+def _heads(name: str, t: torch.Tensor, q: torch.Tensor, shape) -> tuple:
+    """The fields of one sh_heads: t [B, T, heads, d_head] of q's type and device, the last dimension dense."""
     s = t.stride()
-    return t.data_ptr(), s[0], s[1], s[2]
-
-
-def _heads(name: str, t: torch.Tensor, like: torch.Tensor, shape) -> tuple:
-    """The fields of one sh_heads: t [B, T, heads, d_head], the last dimension dense."""
-    s = t.stride()
-    if t.shape != shape or t.dtype != like.dtype or t.get_device() != like.get_device() or (s[3] != 1 and shape[3] > 1):
-        raise ValueError(f"{name} must be [batch, seq, heads, d_head] = {tuple(shape)} of {like.dtype} on {like.device}, its last dimension "
+    if t.shape != shape or t.dtype != q.dtype or t.get_device() != q.get_device() or (s[3] != 1 and shape[3] > 1):
+        raise ValueError(f"{name} must be [batch, seq, heads, d_head] = {tuple(shape)} of {q.dtype} on {q.device}, its last dimension "
                          f"dense: got {tuple(t.shape)}, {t.dtype}, {t.device}, strides {tuple(s)}")
     return t.data_ptr(), s[0], s[1], s[2]
 
 
-def _dense_f32(name: str, t: Optional[torch.Tensor], like: torch.Tensor, shape) -> int:
-    if t is None:
-        return 0
+def _dense_f32(name: str, t: torch.Tensor, like: torch.Tensor, shape) -> int:
     if t.dtype != torch.float32 or t.shape != shape or t.get_device() != like.get_device() or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous fp32 tensor {tuple(shape)} on {like.device}: got {tuple(t.shape)}, {t.dtype}, {t.device}")
     return t.data_ptr()
@@ -400,34 +396,41 @@ def _dense_f32(name: str, t: Optional[torch.Tensor], like: torch.Tensor, shape) 
 
 def _qk_norm_fields(q, k, q_out, k_out, gq, gk, eps, base, rotated, halves, positions, q_scale) -> tuple:
     """The fields of sh_qk_norm_args.  An output that is None is made here; returns (fields, q_out, k_out)."""
-    if q.dim() != 4 or q.dtype not in _DTYPES or not q.is_cuda:
+    code = _DTYPES.get(q.dtype)
+    if code is None or q.dim() != 4 or not q.is_cuda:
         raise ValueError(f"q must be a CUDA tensor [batch, seq, heads, d_head] of fp32, bf16 or fp16: got {tuple(q.shape)}, {q.dtype}, {q.device}")
     shape = q.shape
     B, T, H, D = shape
-    hq = _heads("q", q, q, shape)
+    s = q.stride()
+    if s[3] != 1 and D > 1:
+        raise ValueError(f"q's last dimension must be dense: got strides {s}")
+    hq = (q.data_ptr(), s[0], s[1], s[2])
     if q_out is None:
         q_out = torch.empty_like(q)
-        oq = _strides(q_out)
+        s = q_out.stride()
+        oq = (q_out.data_ptr(), s[0], s[1], s[2])
     else:
         oq = _heads("the output for q", q_out, q, shape)
-    hk, ok, K = _NO_HEADS, _NO_HEADS, 0
-    if k is not None:
+    if k is None:
+        K, hk, ok = 0, _NO_HEADS, _NO_HEADS
+    else:
         ks = k.shape
         K = ks[2] if len(ks) == 4 else 0
         hk = _heads("k", k, q, (B, T, K, D))
         if k_out is None:
             k_out = torch.empty_like(k)
-            ok = _strides(k_out)
+            s = k_out.stride()
+            ok = (k_out.data_ptr(), s[0], s[1], s[2])
         else:
             ok = _heads("the output for k", k_out, q, ks)
     pos = wide = 0
     if positions is not None:
         wide = positions.dtype == torch.int64
-        if positions.shape != (B, T) or not (wide or positions.dtype == torch.int32) or positions.get_device() != q.get_device() or not positions.is_contiguous():
+        if positions.shape != shape[:2] or not (wide or positions.dtype == torch.int32) or positions.get_device() != q.get_device() or not positions.is_contiguous():
             raise ValueError(f"positions must be a contiguous int32 or int64 tensor {(B, T)} on {q.device}: got {tuple(positions.shape)}, {positions.dtype}, {positions.device}")
         pos = positions.data_ptr()
-    return (*hq, *hk, *oq, *ok, _dense_f32("gq", gq, q, (D,)), _dense_f32("gk", gk, q, (D,)), pos, base,
-            _DTYPES[q.dtype], B, T, H, K, D, rotated, halves, wide, eps, q_scale, 0), q_out, k_out
+    return (*hq, *hk, *oq, *ok, 0 if gq is None else _dense_f32("gq", gq, q, (D,)), 0 if gk is None else _dense_f32("gk", gk, q, (D,)), pos, base,
+            code, B, T, H, K, D, rotated, halves, wide, eps, q_scale, 0), q_out, k_out
 
 
 def sh_qk_norm(q: torch.Tensor, k: Optional[torch.Tensor], gq: Optional[torch.Tensor] = None, gk: Optional[torch.Tensor] = None, *, eps: float = 1e-6,
@@ -465,7 +468,7 @@ def sh_qk_norm_backward(q: torch.Tensor, k: Optional[torch.Tensor], dq: torch.Te
     ws, nbytes = None, 0
     if gq is not None or gk is not None:
         nbytes = _qk_norm_workspace_bytes(q.shape[3])
-        ws = torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=q.device)     # (1 us less than torch.empty)
+        ws = (gk if gq is None else gq).new_empty(nbytes // 4)
     _launch(lib.sh_qk_norm_backward, _QK_NORM_BACKWARD.pack(*fields, *_heads("dq", dq, q, q.shape), *(_NO_HEADS if k is None else _heads("dk", dk, q, k.shape)),
                                                             0 if dgq is None else dgq.data_ptr(), 0 if dgk is None else dgk.data_ptr(),
                                                             0 if ws is None else ws.data_ptr(), nbytes), q.get_device())
@@ -500,11 +503,11 @@ def sh_balance_loss(logits: torch.Tensor, idx: torch.Tensor, *, kind: str = "cou
         raise ValueError(f"kind must be one of {sorted(SH_BALANCE)}: got {kind!r}")
     dev = logits.device
     shape, strides, nbytes = _balance_shape(N, S, H, E)
-    loss = torch.empty_strided((), (), dtype=torch.float32, device=dev)
     prob = torch.empty_strided(shape, strides, dtype=torch.float32, device=dev)
+    loss = prob.new_empty(())
     slope = torch.empty_like(prob)
     counts = torch.empty_like(prob, dtype=torch.int32)
-    ws = torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=dev) if nbytes else None
+    ws = prob.new_empty((nbytes + 3) // 4) if nbytes else None
     _launch(lib.sh_balance_loss, _BALANCE.pack(N, logits.stride(0), 0, logits.data_ptr(), idx.data_ptr(), _token_mask(mask, logits), 0, loss.data_ptr(),
                                                prob.data_ptr(), slope.data_ptr(), counts.data_ptr(), 0, ws.data_ptr() if nbytes else 0, nbytes,
                                                _DTYPES[logits.dtype], SH_BALANCE[kind], S, H, E, idx.shape[3], coef, 0), logits.get_device())
@@ -518,13 +521,13 @@ def sh_balance_backward(logits: torch.Tensor, slope: torch.Tensor, *, gloss: Opt
     _logits("logits", logits)
     N, S, H, E = logits.shape
     if out is None:
-        out = torch.empty_like(logits, memory_format=torch.contiguous_format)
+        out = torch.empty_like(logits) if logits.is_contiguous() else torch.empty_like(logits, memory_format=torch.contiguous_format)
     elif out.shape != logits.shape or out.dtype != logits.dtype or out.get_device() != logits.get_device():
         raise ValueError("out must have the shape, type and device of logits")
     else:
         _logits("out", out)
     _launch(lib.sh_balance_backward, _BALANCE.pack(N, logits.stride(0), out.stride(0), logits.data_ptr(), 0, _token_mask(mask, logits),
-                                                   _dense_f32("gloss", gloss, logits, ()), 0, 0, _dense_f32("slope", slope, logits, (S, H, E)), 0,
+                                                   0 if gloss is None else _dense_f32("gloss", gloss, logits, ()), 0, 0, _dense_f32("slope", slope, logits, (S, H, E)), 0,
                                                    out.data_ptr(), 0, 0, _DTYPES[logits.dtype], 0, S, H, E, 1, 0.0, 0), logits.get_device())
     return out
 
@@ -549,7 +552,7 @@ def sh_dropout(x: torch.Tensor, rng: torch.Tensor, p: float, *, residual: Option
     if rng.dtype != torch.int64 or rng.shape != (2,) or rng.get_device() != x.get_device() or not rng.is_contiguous():
         raise ValueError(f"rng must be a contiguous int64 tensor [2] on {x.device}: got {tuple(rng.shape)}, {rng.dtype}, {rng.device}")
     if out is None:
-        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        out = torch.empty_like(x) if x.is_contiguous() else torch.empty_like(x, memory_format=torch.contiguous_format)
     cols = x.shape[-1]
     _launch(lib.sh_dropout, _DROPOUT.pack(x.data_ptr(), 0 if residual is None else residual.data_ptr(), out.data_ptr(), rng.data_ptr(),
                                           x.numel() // cols if cols else 0, cols, _rows("x", x, x), 0 if residual is None else _rows("residual", residual, x),
