@@ -6,6 +6,9 @@
 //
 // A row (a token's E logits of one gate) belongs to L neighbouring lanes with W values each.  Between its rounds a thread
 // stays with the same gate, so its share of P is W sums in registers.
+//
+// What bounds it: instructions (131072 tokens, 8 gates of 32 experts in bf16: sums 24 us - 84 MB, 3.5 TB/s, issue slots two thirds full -, gradient
+// 25 us - 134 MB, 5.4 TB/s); small calls: the latency of their one or two launches.
 #pragma once
 #include <cooperative_groups.h>
 
