@@ -164,6 +164,7 @@ class Layer:
         self.workspace = None
         self.dtype = None
         self.batch = self.seq = 0
+        self._settings, self._of_forward = {}, {}
 
     def sh_configure(self, dtype: int, batch: int, seq: int, device="cuda", cache_len: int = 0) -> None:
         """cache_len > 0: Transformer-XL context (sh_configure_xl): x is [B, cache_len + seq, M], out [B, seq, M]."""
@@ -177,6 +178,8 @@ class Layer:
         self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
         base = self.workspace.data_ptr()
         self._ws_ptr = (base + 255) // 256 * 256
+        self._settings = {}                                # tensors that the training settings read and write, by setting ...
+        self._of_forward = {}                              # ... and those of the last forward pass, which sh_backward differentiates
         _check(lib.sh_set_workspace(self.handle, ctypes.c_void_p(self._ws_ptr), nbytes))
 
     def sh_set_weights(self, Wq, Wk, Wv, Wo, Ws=None, Wd=None, bias_s=None, bias_d=None) -> None:
@@ -213,14 +216,14 @@ class Layer:
         grads = [torch.empty_like(g) if g is not None and train else None for g in (gq, gk)]
         scratch, n = self._scratch(0) if train and eps else (None, 0)
         _check(lib.sh_set_qk_norm(self.handle, _ptr(gq), _ptr(gk), eps, _ptr(grads[0]), _ptr(grads[1]), _ptr(scratch), n))
-        self._qk_norm = (gq, gk, *grads, scratch)          # (the passes read and write them)
+        self._settings["qk_norm"] = (*grads, gq, gk, scratch)
 
     def sh_set_balance(self, kind: Optional[str], coef: float = 0.01, mask: Optional[torch.Tensor] = None, gloss: Optional[torch.Tensor] = None) -> Optional[dict]:
         """sh_forward also gives the balance loss of its gates (fp32 layers): returns the tensors it writes, {loss, counts, prob}; sh_backward
         adds gloss times its gradient to the gates'.  kind: "counts", "entropy", or None to switch it off.  mask [batch * seq] bool: tokens that count."""
         if kind is None:
             _check(lib.sh_set_balance(self.handle, 0, 0.0, *([None] * 6), 0))
-            self._balance = None
+            self._settings.pop("balance", None)
             return None
         dev, (_, H, _, E, _) = self.workspace.device, self.dims
         assert mask is None or (mask.is_cuda and mask.is_contiguous() and mask.dtype in (torch.bool, torch.uint8) and mask.numel() == self.batch * self.seq)
@@ -229,7 +232,7 @@ class Layer:
         out = dict(loss=torch.empty((), device=dev), counts=torch.empty((sides, H, E), dtype=torch.int32, device=dev), prob=torch.empty((sides, H, E), device=dev))
         scratch, n = self._scratch(1)
         _check(lib.sh_set_balance(self.handle, SH_BALANCE[kind], coef, _ptr(mask), _ptr(out["loss"]), _ptr(out["counts"]), _ptr(out["prob"]), _ptr(gloss), _ptr(scratch), n))
-        self._balance = (mask, gloss, out, scratch)
+        self._settings["balance"] = (mask, gloss, out, scratch)
         return out
 
     def sh_set_dropout(self, p: float, rng: Optional[torch.Tensor], train: bool = True) -> None:
@@ -237,7 +240,7 @@ class Layer:
         assert rng is None or (rng.is_cuda and rng.dtype == torch.int64 and rng.is_contiguous() and rng.numel() == 2)
         scratch, n = self._scratch(2) if train and rng is not None else (None, 0)
         _check(lib.sh_set_dropout(self.handle, p, _ptr(rng), _ptr(scratch), n))
-        self._dropout = (rng, scratch)
+        self._settings["dropout"] = (rng, scratch)
 
     def sh_set_output_f16(self, enable: bool) -> None:
         """sh_forward writes fp16 instead of fp32 from now on (bf16 storage configuration only)."""
@@ -249,12 +252,14 @@ class Layer:
         if out is None:
             out = torch.empty((x.shape[0], self.seq_out, x.shape[2]), dtype=getattr(self, "out_dtype", torch.float32), device=x.device)
         assert out.dtype == getattr(self, "out_dtype", torch.float32), "out must have the layer's output dtype (see sh_set_output_f16)"
+        self._of_forward = dict(self._settings)
         _check(lib.sh_forward(self.handle, _ptr(x), _ptr(out), _stream()))
         return out
 
     def sh_forward_timed(self, x: torch.Tensor, out: torch.Tensor):
         """Returns the six stage times in ms: gate+sort, qk, v, attention, o, total."""
         ms = (ctypes.c_float * 6)()
+        self._of_forward = dict(self._settings)
         _check(lib.sh_forward_timed(self.handle, _ptr(x), _ptr(out), _stream(), ms))
         return list(ms)
 
@@ -263,6 +268,7 @@ class Layer:
         nanoseconds of the device clock for the kernels that ran (see STAMP_KERNELS)."""
         n = len(STAMP_KERNELS)
         buf = (ctypes.c_uint64 * (3 * n))()
+        self._of_forward = dict(self._settings)
         _check(lib.sh_forward_stamped(self.handle, _ptr(x), _ptr(out), _stream(), buf))
         return {name: (buf[i], buf[n + i], buf[2 * n + i]) for i, name in enumerate(STAMP_KERNELS) if buf[2 * n + i] != 0}
 
@@ -289,7 +295,7 @@ class Layer:
         g = dict(dx=z(self.batch, self.seq, d_model), dWq=z(H, d_model, D), dWk=z(H, d_model, D), dWv=z(H, E, d_model, D),
                  dWo=z(H, E, D, d_model), dWs=z(H, d_model, E), dWd=z(H, d_model, E))
         _check(lib.sh_backward(self.handle, _ptr(x), _ptr(dout), *[_ptr(g[n]) for n in ("dx", "dWq", "dWk", "dWv", "dWo", "dWs", "dWd")], _stream()))
-        for name, grad in zip(("dgq", "dgk"), getattr(self, "_qk_norm", (None,) * 4)[2:4]):
+        for name, grad in zip(("dgq", "dgk"), self._of_forward.get("qk_norm", ())):
             if grad is not None:
                 g[name] = grad.clone()
         return g

@@ -203,6 +203,26 @@ def test_norm_offsets_past_32_bits():
     torch.cuda.empty_cache()
 
 
+def test_norm_of_more_rows_than_31_bits():
+    # inputs of one row that every token shares (strides of zero), outputs of their own
+    B, T = (1 << 11) + 8, 1 << 20
+    row, drow = torch.randn(1, 1, 1, 2, device="cuda").bfloat16(), torch.randn(1, 1, 1, 2, device="cuda").bfloat16()
+    q = row.expand(B, T, 1, 2)
+    y = torch.empty(B, T, 1, 2, dtype=torch.bfloat16, device="cuda")
+    b.sh_qk_norm(q, None, rotated=2, q_out=y)
+    few = torch.tensor([0, 1, 777, T - 2, T - 1], device="cuda")
+    want, _ = b.sh_qk_norm(row.expand(1, 5, 1, 2), None, rotated=2, positions=few.view(1, 5).int())
+    for n in (0, 1, 1023, 2047, 2048, B - 1):
+        assert torch.equal(y[n, few], want[0]), n
+    del y
+    back = b.sh_qk_norm_backward(q, None, drow.expand(B, T, 1, 2), None, rotated=2)["dq"]
+    want = b.sh_qk_norm_backward(row.expand(1, 5, 1, 2), None, drow.expand(1, 5, 1, 2), None, rotated=2, positions=few.view(1, 5).int())["dq"]
+    for n in (0, 1, 1023, 2047, 2048, B - 1):
+        assert torch.equal(back[n, few], want[0]), n
+    del back
+    torch.cuda.empty_cache()
+
+
 def test_norm_many_rows_take_every_block():
     # more rows than the backward kernel's blocks take in one round, unequal sides
     q, k = draw((4, 2000, 12, 64), torch.bfloat16, 1), draw((4, 2000, 1, 64), torch.bfloat16, 2)

@@ -152,19 +152,50 @@ def test_settings_are_those_of_the_forward_pass_and_can_be_taken_back():
     y = layer.sh_forward(x)
     dset = layer.sh_backward(x, G)
     assert not torch.equal(y, plain)
-    kept = layer._qk_norm, layer._balance, layer._dropout      # (their tensors stay: the pass that was made reads them)
     layer.sh_set_qk_norm(eps=0.0)
     layer.sh_set_balance(None)
     layer.sh_set_dropout(0.0, None)
+    torch.full((1 << 24,), float("nan"), device="cuda")    # (what memory that nobody holds has in it)
     again = layer.sh_backward(x, G)                        # still of the pass that was made
-    for n in ("dx", "dWq", "dWs"):
+    for n in dset:
         assert float((again[n] - dset[n]).abs().max() / dset[n].abs().max()) < 1e-4, n
     back = layer.sh_forward(x)
     assert float((back - plain).abs().max() / plain.abs().max()) < 1e-5
     off_again = layer.sh_backward(x, G)
+    assert set(off_again) == set(dplain)
     for n, w in dplain.items():
         assert float((off_again[n] - w).abs().max() / w.abs().max()) < 1e-4, n
-    assert kept
+    layer.close()
+
+
+def test_other_gains_between_the_passes():
+    cfg = inputs.CONFIGS["tiny_f32"]
+    inp = inputs.make_inputs(cfg)
+    layer = binding.layer_from_inputs(inp)
+    x = binding.to_device(inp.x, cfg.dtype)
+    G = torch.randn_like(x)
+    gains, rng, _, _ = settings(cfg, ("norm", "dropout"))
+    layer.sh_set_rope(10000.0)                             # (before the norms, which take it over)
+    layer.sh_set_qk_norm(*gains, eps=EPS)
+    layer.sh_set_dropout(0.3, rng)
+    layer.sh_forward(x)
+    want = layer.sh_backward(x, G)
+    layer.sh_forward(x)
+    layer.sh_set_qk_norm(torch.zeros(cfg.d_head, device="cuda"), None, eps=EPS)
+    layer.sh_set_dropout(0.9, torch.tensor([5, 5], device="cuda"))
+    layer.sh_set_rope(0.0)
+    for _ in range(8):
+        torch.full((1 << 20,), float("nan"), device="cuda")
+    got = layer.sh_backward(x, G)
+    assert set(got) == set(want)
+    for n in want:
+        assert float((got[n] - want[n]).abs().max() / want[n].abs().max()) < 1e-4, n
+    ref = reference(inp, G.cpu().numpy(), gains=[g.cpu() for g in gains], base=10000.0, drop=op.dropout_kept(64, cfg.d_model, int(rng[0]), int(rng[1]), 0.3))
+    assert off(got["dgq"], ref["dgq"]) < TOL_G and off(got["dx"], ref["dx"]) < TOL_G
+    layer.sh_configure(cfg.dtype, *inp.x.shape[:2])        # no settings any more
+    layer.sh_set_weights(*[binding.to_device(a, cfg.dtype) for a in (inp.Wq, inp.Wk, inp.Wv, inp.Wo, inp.Ws, inp.Wd)])
+    assert off(layer.sh_forward(x), reference(inp, G.cpu().numpy())["y"]) < TOL_Y
+    assert "dgq" not in layer.sh_backward(x, G)
     layer.close()
 
 
