@@ -662,6 +662,8 @@ extern "C" int sh_set_qk_norm(sh_layer* L, const float* gq, const float* gk, flo
   if (eps == 0.f) { L->train.norm = ShQkNorm(); L->train.norm.base = L->rope ? L->rope_base : 0.0; return SH_OK; }
   if (L->moe_q || L->moe_k) { sh_set_error("norms of queries and keys follow the dense Q/K projection: not with query / key experts"); return SH_ERR_UNSUPPORTED; }
   if (L->xl_positions) { sh_set_error("norms of queries and keys do not go with the relative-position term"); return SH_ERR_UNSUPPORTED; }
+  for (const void* g : {(const void*)gq, (const void*)gk, (const void*)dgq, (const void*)dgk})
+    if ((uintptr_t)g % 4) { sh_set_error("gains and their gradients must be aligned to 4 bytes"); return SH_ERR_INVALID_ARG; }
   if ((dgq || dgk) && !scratch) { sh_set_error("gradients of the gains need the scratch"); return SH_ERR_INVALID_ARG; }
   if (int rc = scratch_ok(what, scratch, bytes, sh_f32_norm_scratch(L), true)) return rc;
   ShQkNorm n;
@@ -679,6 +681,8 @@ extern "C" int sh_set_balance(sh_layer* L, int kind, float coef, const void* mas
   if (kind != SH_BALANCE_COUNTS && kind != SH_BALANCE_ENTROPY) { sh_set_error("unknown kind of balance loss: %d", kind); return SH_ERR_INVALID_ARG; }
   if (!(coef - coef == 0.f)) { sh_set_error("coef must be finite (got %g)", (double)coef); return SH_ERR_INVALID_ARG; }
   if (!loss || !counts || !prob) { sh_set_error("loss, counts and prob must not be NULL"); return SH_ERR_INVALID_ARG; }
+  for (const void* g : {(const void*)loss, (const void*)counts, (const void*)prob, (const void*)gloss})
+    if ((uintptr_t)g % 4) { sh_set_error("loss, counts, prob and gloss must be aligned to 4 bytes"); return SH_ERR_INVALID_ARG; }
   if ((long long)L->d.sides * L->d.H > 65535) { sh_set_error("sides * n_heads must be at most 65535"); return SH_ERR_UNSUPPORTED; }
   if (int rc = scratch_ok(what, scratch, bytes, sh_f32_balance_scratch(L), false)) return rc;
   ShBalance b;

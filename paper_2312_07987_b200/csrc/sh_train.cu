@@ -20,6 +20,13 @@ bool dtype_ok(int dtype, bool f16) {
   return false;
 }
 
+// Pointers that a kernel reads or writes as elements of `size` bytes (NULL: not used).
+bool aligned_to(size_t size, const char* what, std::initializer_list<const void*> ptrs) {
+  for (const void* p : ptrs)
+    if ((uintptr_t)p % size) { sh_set_error("%s must be aligned to %zu bytes", what, size); return false; }
+  return true;
+}
+
 // SMs of the current device.
 int device_sms(int* n) {
   static int sms[64];                                      // (an SM count is written once or several times with the same value)
@@ -75,15 +82,16 @@ int qn_check(const sh_qk_norm_args& a, const sh_qk_norm_backward_args* back) {
   if (a.rotated && !(a.base > 0.0 && std::isfinite(a.base))) { sh_set_error("rotary base must be positive and finite (got %g)", a.base); return SH_ERR_INVALID_ARG; }
   if (!(a.eps > 0.f && std::isfinite(a.eps))) { sh_set_error("eps must be positive and finite (got %g)", (double)a.eps); return SH_ERR_INVALID_ARG; }
   if (!std::isfinite(a.q_scale)) { sh_set_error("q_scale must be finite (got %g)", (double)a.q_scale); return SH_ERR_INVALID_ARG; }
+  if (!aligned_to(4, "gains and their gradients", {a.gq, a.gk, back ? back->dgq : nullptr, back ? back->dgk : nullptr})) return SH_ERR_INVALID_ARG;
   if (a.batch == 0 || a.seq == 0) return SH_OK;
+  if (!aligned_to(a.positions_64 ? 8 : 4, "positions", {a.positions})) return SH_ERR_INVALID_ARG;
   struct Side { const char *in, *out; const sh_heads &x, &y; const sh_heads* dy; int heads; };
   const Side sides[2] = {{"q", "q_out", a.q, a.q_out, back ? &back->dq : nullptr, a.q_heads}, {"k", "k_out", a.k, a.k_out, back ? &back->dk : nullptr, a.k_heads}};
   for (const Side& s : sides) {
     if (s.heads == 0) continue;
     if (!s.x.data || !s.y.data) { sh_set_error("%s and %s must not be NULL", s.in, s.out); return SH_ERR_INVALID_ARG; }
     if (s.dy && !s.dy->data) { sh_set_error("d%s must not be NULL", s.in); return SH_ERR_INVALID_ARG; }
-    for (const sh_heads* h : {&s.x, &s.y, s.dy})
-      if (h && (uintptr_t)h->data % elem_bytes(a.dtype)) { sh_set_error("%s, %s or d%s is not aligned to its elements", s.in, s.out, s.in); return SH_ERR_INVALID_ARG; }
+    if (!aligned_to(elem_bytes(a.dtype), "q, k, their outputs and gradients", {s.x.data, s.y.data, s.dy ? s.dy->data : nullptr})) return SH_ERR_INVALID_ARG;
     if (!apart(s.out, {{a.batch, s.y.batch_stride}, {a.seq, s.y.token_stride}, {s.heads, s.y.head_stride}})) return SH_ERR_INVALID_ARG;
   }
   return SH_OK;
@@ -253,6 +261,8 @@ int bl_check(const sh_balance_args& a, bool backward) {
   const long long gates = (long long)a.sides * a.n_heads;
   if (gates > 65535) { sh_set_error("sides * n_heads must be at most 65535 (got %lld)", gates); return SH_ERR_UNSUPPORTED; }
   if (a.n_tokens && !a.logits) { sh_set_error("logits must not be NULL"); return SH_ERR_INVALID_ARG; }
+  if (!aligned_to(elem_bytes(a.dtype), "logits and dlogits", {a.logits, backward ? a.dlogits : nullptr})) return SH_ERR_INVALID_ARG;
+  if (!aligned_to(4, "idx, loss, prob, slope, counts and gloss", {a.idx, a.loss, a.prob, a.slope, a.counts, a.gloss})) return SH_ERR_INVALID_ARG;
   if (backward) {
     if (!a.slope || (a.n_tokens && !a.dlogits)) { sh_set_error("slope and dlogits must not be NULL"); return SH_ERR_INVALID_ARG; }
     return apart("dlogits", {{a.n_tokens, a.dtoken_stride}}) ? SH_OK : SH_ERR_INVALID_ARG;
@@ -384,7 +394,7 @@ int sh_run_dropout(const sh_dropout_args& p, bool pdl, cudaStream_t st) {
   if (p.rows == 0 || p.cols == 0) return SH_OK;
   if (!apart("y", {{p.rows, p.y_stride}})) return SH_ERR_INVALID_ARG;
   if (!p.x || !p.y || !p.rng) { sh_set_error("x, y and rng must not be NULL"); return SH_ERR_INVALID_ARG; }
-  if ((uintptr_t)p.rng % 8) { sh_set_error("rng must be aligned to 8 bytes"); return SH_ERR_INVALID_ARG; }
+  if (!aligned_to(8, "rng", {p.rng}) || !aligned_to(elem_bytes(p.dtype), "x, residual and y", {p.x, p.residual, p.y})) return SH_ERR_INVALID_ARG;
   int sms = 0;
   if (int rc = device_sms(&sms)) return rc;
   const size_t size = elem_bytes(p.dtype);

@@ -130,6 +130,42 @@ def test_norm_and_its_gradients(case, pos):
         close(dg, wg, share * ((TURN_U + NORM_U + 4 + 64 + 256) * U + far), torch.float32)
 
 
+@pytest.mark.parametrize("halves", [False, True])
+def test_norm_gradients_against_differences(halves):
+    # along random directions of x and of the gain: differences of the fp64 definition, 1e-5 to either side (their own error: 1e-10 times third
+    # derivatives of size 10, and 1e-16 / 1e-5 of sums of 1e3), against the kernels' gradients
+    B, T, H, D = 2, 7, 3, 32
+    q, dq = draw((B, T, H, D), torch.float32, 1), draw((B, T, H, D), torch.float32, 2)
+    gain = 1 + 0.3 * torch.randn(D, device="cuda")
+    kw = dict(eps=1e-2, base=100.0, rotated=24, halves=halves)
+    back = b.sh_qk_norm_backward(q, None, dq, None, gain, None, q_scale=0.7, **kw)
+    p = np.broadcast_to(np.arange(T), (B, T))
+    f = lambda x, g: (op.qk_norm(x, g, p, scale=0.7, **kw) * host(dq)).sum()
+    rg = np.random.default_rng(3)
+    for _ in range(3):
+        vx, vg = rg.standard_normal((B, T, H, D)), rg.standard_normal(D)
+        x, g, h = host(q), host(gain), 1e-5
+        size = np.abs(host(dq)).max() * 2.0 / np.sqrt((x * x).mean(-1)).min()
+        slope = (f(x + h * vx, g) - f(x - h * vx, g)) / (2 * h)
+        assert abs((host(back["dq"]) * vx).sum() - slope) < 80 * U * size * np.abs(vx).sum() + 1e-6
+        slope = (f(x, g + h * vg) - f(x, g - h * vg)) / (2 * h)
+        assert abs((host(back["dgq"]) * vg).sum() - slope) < 400 * U * np.abs(host(dq)).max() * 4 * B * T * H * np.abs(vg).max() + 1e-6
+
+
+@pytest.mark.parametrize("kind", ["counts", "entropy"])
+def test_balance_gradient_against_differences(kind):
+    z, idx, mask = balance_inputs(40, 2, 2, 6, 2, torch.float32, True)
+    got = b.sh_balance_loss(z, idx, kind=kind, coef=1.0, mask=mask)
+    dz = host(b.sh_balance_backward(z, got["slope"], mask=mask))
+    f = lambda v: op.balance(v, idx.cpu().numpy(), kind, 1.0, mask.cpu().numpy())[0]
+    rg = np.random.default_rng(4)
+    for _ in range(3):
+        v, h = rg.standard_normal(z.shape), 1e-5
+        slope = (f(host(z) + h * v) - f(host(z) - h * v)) / (2 * h)
+        # (each value: 60 U of p c / n with p <= 1 and c <= 6; the differences: 1e-10 and 1e-16 / 1e-5 of a loss of 24)
+        assert abs((dz * v).sum() - slope) < 60 * U * 6 / int(mask.sum()) * np.abs(v).sum() + 1e-8
+
+
 def test_norm_without_gains_or_keys():
     q, dq = draw((2, 6, 3, 40), torch.float32, 1), draw((2, 6, 3, 40), torch.float32, 2)
     y, none = b.sh_qk_norm(q, None, rotated=40)

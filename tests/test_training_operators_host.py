@@ -33,7 +33,7 @@ def norm_args(heads=None, backward=False, **kw):
     (dict(d_head=33, rotated=32), {}, -2, "even d_head"), (dict(base=0.0), {}, -1, "base"), (dict(base=float("nan")), {}, -1, "base"), (dict(eps=0.0), {}, -1, "eps"),
     (dict(eps=float("nan")), {}, -1, "eps"), (dict(q_scale=float("inf")), {}, -1, "q_scale"), (dict(q_heads=-1), {}, -1, "heads"), ({}, dict(k=dict(data=0)), -1, "k and k_out"),
     ({}, dict(q_out=dict(data=0)), -1, "q_out"), ({}, dict(k_out=dict(token_stride=0)), -1, "share an address"), ({}, dict(q_out=dict(head_stride=0)), -1, "share an address"),
-    ({}, dict(q=dict(data=PTR + 2)), -1, "not aligned"),
+    ({}, dict(q=dict(data=PTR + 2)), -1, "aligned to 4"), (dict(gq=PTR + 2), {}, -1, "gains"), (dict(positions=PTR + 4, positions_64=1), {}, -1, "positions"),
 ])
 def test_norm_refusals(kw, heads, code, frag):
     for fn, backward in ((b.lib.sh_qk_norm, False), (b.lib.sh_qk_norm_backward, True)):
@@ -69,14 +69,14 @@ def balance_args(**kw):
     (dict(dtype=b.SH_F16), -1, "dtype"), (dict(n_tokens=-1), -1, "n_tokens"), (dict(sides=0), -1, "sides"), (dict(n_heads=0), -1, "n_heads"), (dict(n_experts=33), -1, "n_experts"),
     (dict(sides=256, n_heads=256), -2, "65535"), (dict(logits=0), -1, "logits"), (dict(k=0), -1, "k must"), (dict(k=5), -1, "k must"), (dict(n_tokens=1 << 30), -2, "2^31"),
     (dict(kind=2), -1, "kind"), (dict(coef=float("nan")), -1, "coef"), (dict(idx=0), -1, "idx"), (dict(loss=0), -1, "loss"), (dict(counts=0), -1, "counts"),
-    (dict(workspace=0), -4, "workspace"), (dict(workspace=PTR + 16), -4, "256"), (dict(workspace_bytes=100), -4, "too small"),
+    (dict(logits=PTR + 2), -1, "logits"), (dict(idx=PTR + 1), -1, "idx"), (dict(prob=PTR + 2), -1, "prob"), (dict(workspace=0), -4, "workspace"), (dict(workspace=PTR + 16), -4, "256"), (dict(workspace_bytes=100), -4, "too small"),
 ])
 def test_balance_refusals(kw, code, frag):
     assert b.lib.sh_balance_loss(balance_args(**kw), None) == code
     assert frag in b.sh_last_error()
 
 
-@pytest.mark.parametrize("kw,frag", [(dict(slope=0), "slope"), (dict(dlogits=0), "dlogits"), (dict(dtoken_stride=0), "share an address"), (dict(dtype=7), "dtype"), (dict(logits=0), "logits")])
+@pytest.mark.parametrize("kw,frag", [(dict(slope=0), "slope"), (dict(dlogits=0), "dlogits"), (dict(dtoken_stride=0), "share an address"), (dict(dtype=7), "dtype"), (dict(logits=0), "logits"), (dict(dlogits=PTR + 2), "dlogits"), (dict(gloss=PTR + 1), "gloss")])
 def test_balance_backward_refusals(kw, frag):
     assert b.lib.sh_balance_backward(balance_args(**kw), None) == -1
     assert frag in b.sh_last_error()
@@ -91,7 +91,8 @@ def test_balance_workspace():
 
 @pytest.mark.parametrize("kw,code,frag", [
     (dict(dtype=5), -1, "dtype"), (dict(rows=-1), -1, "rows"), (dict(cols=-1), -1, "cols"), (dict(cols=1 << 31), -2, "cols"), (dict(rows=(1 << 32) + 1), -2, "rows"), (dict(p=-0.1), -1, "p must"),
-    (dict(p=1.5), -1, "p must"), (dict(p=float("nan")), -1, "p must"), (dict(x=0), -1, "x, y"), (dict(y=0), -1, "x, y"), (dict(rng=0), -1, "rng"), (dict(rng=PTR + 4), -1, "rng"),
+    (dict(p=1.5), -1, "p must"), (dict(p=float("nan")), -1, "p must"), (dict(x=0), -1, "x, y"), (dict(y=0), -1, "x, y"), (dict(rng=0), -1, "rng"), (dict(rng=PTR + 4), -1, "rng"), (dict(x=PTR + 2), -1, "aligned"),
+    (dict(residual=PTR + 1), -1, "aligned"),
     (dict(y_stride=0), -1, "share an address"),
 ])
 def test_dropout_refusals(kw, code, frag):
@@ -111,3 +112,47 @@ def test_binding_refuses_host_tensors():
         b.sh_balance_backward(x, x)
     with pytest.raises(ValueError, match="CUDA"):
         b.sh_dropout(x, torch.zeros(2, dtype=torch.int64), 0.1)
+
+
+def configured(dtype=b.SH_F32, **kw):
+    import ctypes
+    h = ctypes.c_void_p(b.lib.sh_create(128, 2, 32, 4, 2) if not kw else b.lib.sh_create_moe_qk(128, 2, 32, 4, 2, 1, 1, 0))
+    assert b.lib.sh_configure(h, dtype, 2, 64) == 0
+    return h
+
+
+def test_layer_settings_refusals():
+    lib, P = b.lib, PTR * 16
+    bare = configured()
+    assert lib.sh_training_scratch_bytes(None, 0) == 0
+    assert lib.sh_set_qk_norm(None, None, None, 1e-6, None, None, None, 0) == -1
+    for call in (lambda h: lib.sh_set_qk_norm(h, None, None, 1e-6, None, None, None, 0), lambda h: lib.sh_set_balance(h, 0, 1.0, None, P, P, P, None, P, 1 << 30),
+                 lambda h: lib.sh_set_dropout(h, 0.1, P, None, 0)):
+        assert call(bare) == -3 and "workspace" in b.sh_last_error()                  # no workspace yet
+        bf = configured(b.SH_BF16)
+        assert lib.sh_set_workspace(bf, P, lib.sh_workspace_bytes(bf)) == 0
+        assert call(bf) == -2 and "fp32" in b.sh_last_error()
+        lib.sh_destroy(bf)
+    assert lib.sh_set_workspace(bare, P, lib.sh_workspace_bytes(bare)) == 0
+    need = [lib.sh_training_scratch_bytes(bare, i) for i in range(4)]
+    assert all(n > 0 for n in need[:3]) and need[3] == 0
+    norm = lambda gq=None, gk=None, eps=1e-6, dgq=None, dgk=None, s=None, n=0: lib.sh_set_qk_norm(bare, gq, gk, eps, dgq, dgk, s, n)
+    for args, code, frag in ((dict(eps=-1.0), -1, "eps"), (dict(eps=float("nan")), -1, "eps"), (dict(gq=P + 2), -1, "aligned"), (dict(dgq=P), -1, "scratch"),
+                             (dict(s=P + 8, n=1 << 30), -4, "256"), (dict(s=P, n=need[0] - 1), -4, "too small")):
+        assert norm(**args) == code and frag in b.sh_last_error(), args
+    assert norm(s=P, n=need[0]) == 0 and norm(eps=0.0) == 0
+    bal = lambda kind=0, coef=1.0, loss=P, counts=P, prob=P, s=P, n=1 << 30: lib.sh_set_balance(bare, kind, coef, None, loss, counts, prob, None, s, n)
+    for args, code, frag in ((dict(kind=5), -1, "kind"), (dict(coef=float("inf")), -1, "coef"), (dict(loss=None), -1, "loss"), (dict(counts=P + 1), -1, "aligned"),
+                             (dict(s=None), -4, "scratch"), (dict(n=need[1] - 1), -4, "too small")):
+        assert bal(**args) == code and frag in b.sh_last_error(), args
+    assert bal() == 0 and bal(loss=None, s=None) == 0
+    drop = lambda p=0.1, rng=P, s=None, n=0: lib.sh_set_dropout(bare, p, rng, s, n)
+    for args, code, frag in ((dict(p=1.1), -1, "p must"), (dict(p=float("nan")), -1, "p must"), (dict(rng=P + 4), -1, "rng"), (dict(s=P + 1, n=1 << 30), -4, "256"),
+                             (dict(s=P, n=need[2] - 1), -4, "too small")):
+        assert drop(**args) == code and frag in b.sh_last_error(), args
+    assert drop(s=P, n=need[2]) == 0 and drop(rng=None) == 0
+    moe = configured(moe=True)
+    assert lib.sh_set_workspace(moe, P, lib.sh_workspace_bytes(moe)) == 0
+    assert lib.sh_set_qk_norm(moe, None, None, 1e-6, None, None, None, 0) == -2 and "experts" in b.sh_last_error()
+    lib.sh_destroy(moe)
+    lib.sh_destroy(bare)
