@@ -559,6 +559,29 @@ def test_captured_calls_replay_on_new_inputs():
             assert all(torch.equal(a, c) for a, c in zip(out, want)), turn
 
 
+def test_two_calls_at_once():
+    q, dq, g = torch.randn(4, 300, 6, 64, device="cuda"), torch.randn(4, 300, 6, 64, device="cuda"), torch.randn(64, device="cuda")
+    z, idx, _ = balance_inputs(9001, 2, 2, 16, 3, torch.float32, False)
+    x, rng = torch.randn(3000, 77, device="cuda"), torch.tensor([1, 1], device="cuda")
+
+    def calls():
+        back = b.sh_qk_norm_backward(q, q, dq, dq, g, g, rotated=64)
+        got = b.sh_balance_loss(z, idx, kind="entropy")
+        return [*back.values(), *got.values(), b.sh_balance_backward(z, got["slope"]), b.sh_dropout(x, rng, 0.5)]
+
+    want = calls()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    outs = []
+    for _ in range(10):
+        for s in streams:
+            with torch.cuda.stream(s):
+                outs.append(calls())
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, w) for out in outs for a, w in zip(out, want))
+
+
 def test_on_another_stream():
     side = torch.cuda.Stream()
     x = torch.zeros(1 << 24, device="cuda").view(1 << 12, 1 << 12)
