@@ -148,25 +148,46 @@ __device__ __forceinline__ void bl_sums(const BlArgs& a, int block, int blocks, 
   __syncthreads();
 }
 
+// The block's sum of p of every (gate, expert) from its rows' sums, in 64 bits: a gate that is nearly balanced has a gradient of
+// what is left of ln P behind its mean, and 256 sums of a size added in 32 bits cost it 5 of its 24 bits.  All threads, then those of the
+// columns, in a fixed order.
+template <int THREADS, int LD, typename F>
+__device__ __forceinline__ void bl_columns(const BlArgs& a, int ng, const float (*s_p)[LD], double* s_part, F store) {
+  const int cols = ng * a.E, parts = cols < THREADS ? THREADS / cols : 1;
+  for (int c0 = 0; c0 < cols; c0 += THREADS) {             // (one round where parts > 1)
+    const int i = threadIdx.x % (parts > 1 ? cols : THREADS), part = parts > 1 ? threadIdx.x / cols : 0, c = c0 + i;
+    double sum = 0.0;
+    if (part < parts && c < cols) {
+      const int q = c / a.E, e = c % a.E;
+      for (int k = part; k < a.tpb; k += parts) sum += (double)s_p[k * a.per + q][e];
+      s_part[threadIdx.x] = sum;
+    }
+    __syncthreads();
+    if (part == 0 && c < cols) {
+      for (int k = 1; k < parts; ++k) sum += s_part[k * cols + i];
+      store(c, sum);
+    }
+    __syncthreads();
+  }
+}
+
 template <typename T, int W, int L, bool VEC>
 static __global__ void __launch_bounds__(BL_THREADS, BL_BLOCKS) sh_balance_sums_kernel(const BlArgs a) {
   constexpr int EP = W * L, ROWS = BL_THREADS / L;
   __shared__ float s_p[ROWS][EP + 1];
   __shared__ int s_n[ROWS * EP];                         // [gate of the block][expert]
+  __shared__ double s_part[BL_THREADS];
   __shared__ int s_tokens;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.ticket = 0;
   const int g0 = blockIdx.y * a.per, ng = min(a.per, a.gates - g0);
   bl_sums<T, W, L, VEC, BL_THREADS>(a, blockIdx.x, gridDim.x, g0, ng, s_p, s_n, &s_tokens);
-  const long long base = (long long)blockIdx.x * a.gates * a.E;
-  for (int i = threadIdx.x; i < ng * a.E; i += BL_THREADS) {
-    const int q = i / a.E, e = i % a.E;
-    float sum = 0.f;
-    for (int k = 0; k < a.tpb; ++k) sum += s_p[k * a.per + q][e];
-    a.part_p[base + (long long)(g0 + q) * a.E + e] = sum;
-    a.part_n[base + (long long)(g0 + q) * a.E + e] = s_n[q * EP + e];
-  }
+  const long long base = (long long)blockIdx.x * a.gates * a.E + (long long)g0 * a.E;
+  bl_columns<BL_THREADS, EP + 1>(a, ng, s_p, s_part, [&](int c, double sum) {
+    a.part_p[base + c] = (float)sum;                       // (hundreds of them, each rounded by itself)
+    a.part_n[base + c] = s_n[c / a.E * EP + c % a.E];
+  });
   if (blockIdx.y == 0 && threadIdx.x == 0) a.part_n[(long long)gridDim.x * a.gates * a.E + blockIdx.x] = s_tokens;
 }
 
@@ -254,16 +275,16 @@ static __global__ void __launch_bounds__(BL_LOSS_THREADS) sh_balance_loss_kernel
 }
 
 // Both in one launch, for few rows: a cluster of 8 blocks, whose sums are read over distributed shared memory, a warp to a gate.
-// (Such calls are bound by their launches: 2048 tokens, 8 gates of 4 experts, 13.8 us a call, 17.4 with the two kernels.)
+// (Such calls are bound by their launches: 2048 tokens, 8 gates of 4 experts, 14.2 us a call, 17.6 with the two kernels.)
 constexpr int BL_SMALL_THREADS = 512, BL_CLUSTER = 8;
-constexpr int BL_SMALL_COLS = 1024, BL_SMALL_GATES = 64;   // gates * experts, gates at most
+constexpr int BL_SMALL_COLS = 512, BL_SMALL_GATES = 64;   // gates * experts, gates at most
 template <typename T, int W, int L, bool VEC>
 static __global__ void __launch_bounds__(BL_SMALL_THREADS, 1) sh_balance_small_kernel(const BlArgs a, const BlOut o) {
   namespace cg = cooperative_groups;
   constexpr int EP = W * L, ROWS = BL_SMALL_THREADS / L;
   __shared__ float s_p[ROWS][EP + 1];
   __shared__ int s_n[BL_SMALL_GATES * EP < 2 * BL_SMALL_COLS ? BL_SMALL_GATES * EP : 2 * BL_SMALL_COLS];
-  __shared__ float s_sum[BL_SMALL_COLS];
+  __shared__ double s_sum[BL_SMALL_COLS], s_part[BL_SMALL_THREADS];
   __shared__ double s_loss[BL_SMALL_GATES];
   __shared__ int s_tokens;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -271,12 +292,7 @@ static __global__ void __launch_bounds__(BL_SMALL_THREADS, 1) sh_balance_small_k
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank();
   bl_sums<T, W, L, VEC, BL_SMALL_THREADS>(a, rank, BL_CLUSTER, 0, a.gates, s_p, s_n, &s_tokens);
-  for (int i = threadIdx.x; i < a.gates * a.E; i += BL_SMALL_THREADS) {
-    const int q = i / a.E, e = i % a.E;
-    float sum = 0.f;
-    for (int k = 0; k < a.tpb; ++k) sum += s_p[k * a.per + q][e];
-    s_sum[i] = sum;
-  }
+  bl_columns<BL_SMALL_THREADS, EP + 1>(a, a.gates, s_p, s_part, [&](int c, double sum) { s_sum[c] = sum; });
   cluster.sync();
   const int e = threadIdx.x & 31;
   for (int gate = rank + BL_CLUSTER * (threadIdx.x >> 5); gate < a.gates; gate += BL_CLUSTER * (BL_SMALL_THREADS / 32)) {
@@ -285,7 +301,7 @@ static __global__ void __launch_bounds__(BL_SMALL_THREADS, 1) sh_balance_small_k
 #pragma unroll
     for (int b = 0; b < BL_CLUSTER; ++b) {
       if (e < a.E) {
-        p += (double)cluster.map_shared_rank(s_sum, b)[gate * a.E + e];
+        p += cluster.map_shared_rank(s_sum, b)[gate * a.E + e];
         n += cluster.map_shared_rank(s_n, b)[gate * EP + e];
       }
       tokens += *cluster.map_shared_rank(&s_tokens, b);

@@ -360,6 +360,24 @@ def test_balance_of_two_launches(N, S, H, E, ty, kind):
     close(dz, host(want), host(p) * 0.1 * (2 * (E if kind == "counts" else 1 + log) * (p_u + 16 * U) + 2 * P_u) / n, TYPES[ty])
 
 
+@pytest.mark.parametrize("N,S,H,E", [(2010, 2, 4, 2), (100000, 1, 2, 3), (4000, 1, 1, 4)])
+def test_balance_of_nearly_balanced_gates(N, S, H, E):
+    """The entropy's slope is what is left of ln P behind its mean: P has to be exact far below a rounding of its size a token."""
+    g = torch.Generator(device="cuda").manual_seed(N)
+    z = torch.randn(N, S, H, E, generator=g, device="cuda")
+    idx = torch.zeros(S, N, H, 1, dtype=torch.int32, device="cuda")
+    got = b.sh_balance_loss(z, idx, kind="entropy")
+    dz = b.sh_balance_backward(z, got["slope"])
+    p = torch.softmax(z.double(), -1)
+    c = torch.log(p.mean(0))
+    want = p * (c - (p * c).sum(-1, keepdim=True)) / N
+    spread = float((c - c.mean(-1, keepdim=True)).square().mean().sqrt())
+    # p: 30 U a token, by roundings of its own: six standard deviations of their mean 180 U / sqrt(N), beside blocks' sums rounded once each
+    # (8 or more: U); as a share of the slope's spread, and 40 U of the products
+    rel = float((dz.double() - want).norm() / want.norm())
+    assert rel < (180 / np.sqrt(N) + 1) * U / spread + 40 * U, (rel, spread)
+
+
 @pytest.mark.parametrize("kind", ["counts", "entropy"])
 def test_balance_extreme_logits(kind):
     z, idx, mask = balance_inputs(64, 2, 2, 8, 2, torch.float32, False)
