@@ -331,14 +331,13 @@ size_t sh_qk_norm_workspace_bytes(int d_head);
  *   SH_BALANCE_ENTROPY:  loss = coef * sum over the gates of  sum_e P_e ln P_e         (the negative entropy of the mean)
  * A negative entry of idx (or one that is no expert) is not counted.  A row of -inf only has p = 0.  No token that counts:
  * everything is zero.
- *   loss [1], prob, slope [sides, H, E] fp32, counts [sides, H, E] int32; slope = dloss/dprob / n, less its mean over the
+ *   loss [1], prob, slope [sides, H, E] fp32, counts [sides, H, E] int32 (sums in 64 bits); slope = dloss/dprob / n, less its mean over the
  *   gate's experts (which changes no gradient), is what sh_balance_backward reads.
  * sh_balance_backward: dlogits = *gloss * dloss/dlogits (gloss: device, NULL: 1), in the type of the logits, tokens
  * dtoken_stride elements apart; the counts are constants of it.  Tokens that do not count get zeros.  Reads logits, mask,
  * slope; dlogits may be logits itself (same stride).
  * workspace: sh_balance_workspace_bytes(N, sides, H, E) bytes aligned to 256 (sh_balance_loss only; 0: few rows, NULL will do).
- * 1 <= k <= E <= 32; N * k
- * below 2^31.  The same inputs give the same bits. */
+ * 1 <= k <= E <= 32; N * k below 2^31.  The same inputs give the same bits. */
 enum { SH_BALANCE_COUNTS = 0, SH_BALANCE_ENTROPY = 1 };
 typedef struct {
   int64_t n_tokens, token_stride, dtoken_stride;
@@ -381,10 +380,11 @@ int sh_dropout(const sh_dropout_args* args, void* stream);
 
 /* The same as parts of the fp32 layer's own passes.  Host calls, no launch; they take effect with the next sh_forward, and end with
  * sh_configure / sh_set_workspace.  All pointers are device pointers of the caller, read or written by the passes: they stay
- * valid as long as the setting does, and until the last forward pass that had it has been differentiated (or another one made).  A scratch holds sh_training_scratch_bytes(layer, which) bytes, aligned to 256, of one
- * layer; sh_backward reads what the forward pass left there (without it - where it may be NULL - sh_backward has no pass to
- * differentiate).  sh_backward differentiates the pass that was made, with its settings.  SH_ERR_UNSUPPORTED for bf16
- * storage and the dense comparator. */
+ * valid as long as the setting does, and until the last forward pass that had it has been differentiated (or another one
+ * made).  A scratch holds sh_training_scratch_bytes(layer, which) bytes, aligned to 256, of one layer; sh_backward reads what
+ * the forward pass left there (without it - where it may be NULL - sh_backward has no pass to differentiate).  sh_backward
+ * differentiates the pass that was made, with its settings.  SH_ERR_UNSUPPORTED for bf16 storage and the dense
+ * comparator. */
 enum { SH_SCRATCH_QK_NORM = 0, SH_SCRATCH_BALANCE = 1, SH_SCRATCH_DROPOUT = 2 };
 size_t sh_training_scratch_bytes(const sh_layer* layer, int which);     /* 0: not configured, or not such a layer */
 

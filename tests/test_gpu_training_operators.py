@@ -96,12 +96,9 @@ def positions_for(kind, B, T):
     return torch.from_numpy(p.astype(np.int32 if kind != "far" else np.int64)).cuda(), p
 
 
-@pytest.mark.parametrize("pos", ["none", "packed", "far", "negative"])
-@pytest.mark.parametrize("case", CASES)
+@pytest.mark.parametrize("case,pos", [(c, pos) for c in CASES for pos in (("none", "packed", "far", "negative") if c[5] else ("none",))])
 def test_norm_and_its_gradients(case, pos):
     B, T, Hq, Hk, D, R, halves, layout, ty, qs = case
-    if pos != "none" and R == 0:
-        pytest.skip("nothing is rotated")
     t = TYPES[ty]
     q, k = draw((B, T, Hq, D), t, 1, layout, Hk), draw((B, T, Hk, D), t, 2, layout, Hq)
     dq, dk = draw((B, T, Hq, D), t, 3), draw((B, T, Hk, D), t, 4, "bhtd")
@@ -548,14 +545,15 @@ def test_captured_calls_replay_on_new_inputs():
     q, k = torch.randn(2, 40, 4, 64, device="cuda"), torch.randn(2, 40, 2, 64, device="cuda")
     dq, dk, gain = torch.randn_like(q), torch.randn_like(k), torch.ones(64, device="cuda")
     z, idx, _ = balance_inputs(80, 2, 2, 8, 2, torch.float32, False)
+    large, lidx, _ = balance_inputs(9001, 1, 2, 16, 2, torch.bfloat16, False)
     x, rng = torch.randn(80, 128, device="cuda"), torch.tensor([1, 1], device="cuda")
 
     def calls():
         y = b.sh_qk_norm(q, k, gain, gain, rotated=64)
         back = b.sh_qk_norm_backward(q, k, dq, dk, gain, gain, rotated=64)
-        got = b.sh_balance_loss(z, idx, kind="entropy")
+        got, more = b.sh_balance_loss(z, idx, kind="entropy"), b.sh_balance_loss(large, lidx)
         dz = b.sh_balance_backward(z, got["slope"], gloss=got["loss"])
-        return [*y, *back.values(), *got.values(), dz, b.sh_dropout(x, rng, 0.5, residual=x)]
+        return [*y, *back.values(), *got.values(), dz, *more.values(), b.sh_dropout(x, rng, 0.5, residual=x), b.sh_dropout(x.view(-1)[:10001], rng, 0.5)]
 
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
@@ -567,7 +565,7 @@ def test_captured_calls_replay_on_new_inputs():
         with torch.cuda.graph(g):
             outs.append(calls())
     for turn in range(3):
-        for a in (q, k, dq, dk, z, x):
+        for a in (q, k, dq, dk, z, x, large):
             a.normal_()
         rng[1] += 1
         want = calls()
