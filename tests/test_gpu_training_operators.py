@@ -480,6 +480,9 @@ def test_dropout_rows_apart(stride, cols, ty):
     assert torch.equal(b.sh_dropout(view, rng, 0.3), plain)
     assert b.sh_dropout(view, rng, 0.3, residual=res, out=view) is view
     assert torch.equal(view, want) and (wide[:, cols:] == 5).all()
+    one = res[:1].expand(rows, cols)                                                        # one row for all of them
+    assert torch.equal(b.sh_dropout(x, rng, 0.3, residual=one), b.sh_dropout(x, rng, 0.3, residual=one.contiguous()))
+    assert torch.equal(b.sh_dropout(x[:1].expand(rows, cols), rng, 0.3), b.sh_dropout(x[:1].repeat(rows, 1), rng, 0.3))
     off = torch.empty(rows * cols + 1, device="cuda", dtype=t)[1:].view(rows, cols)         # dense, one value off alignment
     off.copy_(x)
     assert torch.equal(b.sh_dropout(off, rng, 0.3), plain)
