@@ -400,6 +400,17 @@ def _dense_f32(name: str, t: torch.Tensor, like: torch.Tensor, shape) -> int:
     return t.data_ptr()
 
 
+def _heads_like(t: torch.Tensor) -> tuple:
+    """An output for t [B, T, heads, d_head] and its fields: t's order of dimensions, but the last one dense (for an input whose rows overlap -
+    windows of one buffer, say - empty_like may put another dimension innermost)."""
+    out = torch.empty_like(t)
+    s = out.stride()
+    if s[3] != 1 and t.shape[3] > 1:
+        out = torch.empty_like(t, memory_format=torch.contiguous_format)
+        s = out.stride()
+    return out, (out.data_ptr(), s[0], s[1], s[2])
+
+
 def _qk_norm_fields(q, k, q_out, k_out, gq, gk, eps, base, rotated, halves, positions, q_scale) -> tuple:
     """The fields of sh_qk_norm_args.  An output that is None is made here; returns (fields, q_out, k_out)."""
     code = _DTYPES.get(q.dtype)
@@ -412,9 +423,7 @@ def _qk_norm_fields(q, k, q_out, k_out, gq, gk, eps, base, rotated, halves, posi
         raise ValueError(f"q's last dimension must be dense: got strides {s}")
     hq = (q.data_ptr(), s[0], s[1], s[2])
     if q_out is None:
-        q_out = torch.empty_like(q)
-        s = q_out.stride()
-        oq = (q_out.data_ptr(), s[0], s[1], s[2])
+        q_out, oq = _heads_like(q)
     else:
         oq = _heads("the output for q", q_out, q, shape)
     if k is None:
@@ -424,9 +433,7 @@ def _qk_norm_fields(q, k, q_out, k_out, gq, gk, eps, base, rotated, halves, posi
         K = ks[2] if len(ks) == 4 else 0
         hk = _heads("k", k, q, (B, T, K, D))
         if k_out is None:
-            k_out = torch.empty_like(k)
-            s = k_out.stride()
-            ok = (k_out.data_ptr(), s[0], s[1], s[2])
+            k_out, ok = _heads_like(k)
         else:
             ok = _heads("the output for k", k_out, q, ks)
     pos = wide = 0

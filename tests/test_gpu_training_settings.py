@@ -1,0 +1,31 @@
+"""Calls of the training operators and of the layer's training settings in combinations that their own tests do not make: inputs
+whose rows overlap, settings switched between the passes, refused calls, a cache, and sizes above the small kernels' limits."""
+import pytest
+import torch
+
+from paper_2312_07987_b200 import binding
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+@pytest.mark.parametrize("strides", [(100, 1, 40, 1), (1, 1, 1, 1), (0, 3, 0, 1), (200, 8, 0, 1)])
+def test_norm_of_rows_that_overlap(strides):
+    """Inputs may share addresses (windows of one buffer, one row for all heads): what a copy of their own gives."""
+    q = torch.randn(400, device="cuda").as_strided((2, 3, 2, 8), strides)
+    dq = torch.randn(400, device="cuda").as_strided((2, 3, 2, 8), strides[2::-1] + (1,))
+    gain = torch.randn(8, device="cuda")
+    own, down = q.contiguous(), dq.contiguous()
+    kw = dict(rotated=8, halves=True, q_scale=0.5)
+    y, yk = binding.sh_qk_norm(q, q, gain, gain, **kw)
+    want, wantk = binding.sh_qk_norm(own, own, gain, gain, **kw)
+    assert y.stride(3) == yk.stride(3) == 1
+    back, bwant = binding.sh_qk_norm_backward(q, q, dq, dq, gain, gain, **kw), binding.sh_qk_norm_backward(own, own, down, down, gain, gain, **kw)
+    # Vectors are as wide as the addresses allow, so sums may go in another order.  A normalised value is at most sqrt(8) and its row's mean
+    # magnitude at most 1; a result of either side is off by 40 roundings of these (sum, root, angle, products), a gradient by 80 of its terms
+    # w (1 + sqrt(8)) / size, w the turned gradient times its gain, a gain's gradient by 100 of each of its 12 rows' terms.
+    g, d = float(gain.abs().max()), 2 ** 0.5 * float(down.abs().max())
+    size = float(own.square().mean(-1).sqrt().min())
+    for got, ref, bound in ((y, want, 40 * 4 * g), (yk, wantk, 40 * 4 * g), (back["dq"], bwant["dq"], 80 * 4 * d * g / size), (back["dk"], bwant["dk"], 80 * 4 * d * g / size),
+                            (back["dgq"], bwant["dgq"], 100 * 12 * 3 * d), (back["dgk"], bwant["dgk"], 100 * 12 * 3 * d)):
+        assert float((got - ref).abs().max()) <= 2 * U * bound
