@@ -213,8 +213,14 @@ class Layer:
         D = self.dims[2]
         for g in (gq, gk):
             assert g is None or (g.is_cuda and g.is_contiguous() and g.dtype == torch.float32 and tuple(g.shape) == (D,))
+        if ctypes.c_float(eps).value == 0.0:               # (as the call takes it; off: no gains, so no gradients of them)
+            if eps != 0.0:
+                raise ValueError(f"eps must be 0 (off) or at least fp32's smallest positive value: got {eps}")
+            _check(lib.sh_set_qk_norm(self.handle, None, None, 0.0, None, None, None, 0))
+            self._settings.pop("qk_norm", None)
+            return
         grads = [torch.empty_like(g) if g is not None and train else None for g in (gq, gk)]
-        scratch, n = self._scratch(0) if train and eps else (None, 0)
+        scratch, n = self._scratch(0) if train else (None, 0)
         _check(lib.sh_set_qk_norm(self.handle, _ptr(gq), _ptr(gk), eps, _ptr(grads[0]), _ptr(grads[1]), _ptr(scratch), n))
         self._settings["qk_norm"] = (*grads, gq, gk, scratch)
 

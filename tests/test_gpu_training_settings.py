@@ -3,7 +3,7 @@ whose rows overlap, settings switched between the passes, refused calls, a cache
 import pytest
 import torch
 
-from paper_2312_07987_b200 import binding
+from paper_2312_07987_b200 import binding, inputs
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
@@ -29,3 +29,28 @@ def test_norm_of_rows_that_overlap(strides):
     for got, ref, bound in ((y, want, 40 * 4 * g), (yk, wantk, 40 * 4 * g), (back["dq"], bwant["dq"], 80 * 4 * d * g / size), (back["dk"], bwant["dk"], 80 * 4 * d * g / size),
                             (back["dgq"], bwant["dgq"], 100 * 12 * 3 * d), (back["dgk"], bwant["dgk"], 100 * 12 * 3 * d)):
         assert float((got - ref).abs().max()) <= 2 * U * bound
+
+
+def tiny_layer():
+    inp = inputs.make_inputs(inputs.CONFIGS["tiny_f32"])
+    return binding.layer_from_inputs(inp), binding.to_device(inp.x, inp.cfg.dtype)
+
+
+def test_norms_switched_off_with_their_gains():
+    """eps = 0 is off whatever else is given: a plain pass, and no gradients of gains that were not used."""
+    layer, x = tiny_layer()
+    G = torch.randn_like(x)
+    plain, dplain = layer.sh_forward(x), layer.sh_backward(x, G)
+    gains = [torch.full((layer.dims[2],), 1.5, device="cuda") for _ in range(2)]
+    layer.sh_set_qk_norm(*gains)
+    layer.sh_forward(x)
+    assert {"dgq", "dgk"} < set(layer.sh_backward(x, G))
+    layer.sh_set_qk_norm(*gains, eps=0.0)
+    assert float((layer.sh_forward(x) - plain).abs().max() / plain.abs().max()) < 1e-5
+    back = layer.sh_backward(x, G)
+    assert set(back) == set(dplain)
+    for n, w in dplain.items():
+        assert float((back[n] - w).abs().max() / w.abs().max()) < 1e-4, n
+    with pytest.raises(ValueError, match="eps"):
+        layer.sh_set_qk_norm(*gains, eps=1e-46)
+    layer.close()

@@ -22,3 +22,48 @@ def test_outputs_of_heads_keep_the_order_of_dimensions():
     for t in (torch.zeros(2, 5, 3, 8), torch.zeros(2, 3, 5, 8).transpose(1, 2)):
         out, fields = b._heads_like(t)
         assert out.stride() == t.stride() and fields == (out.data_ptr(), *t.stride()[:3])
+
+
+class OnDevice(torch.Tensor):
+    """A host tensor that passes for one on the device: what calls it is a stand-in for the library."""
+    is_cuda = True
+
+
+def device_tensor(*shape, dtype=torch.float32):
+    return torch.zeros(*shape, dtype=dtype).as_subclass(OnDevice)
+
+
+@pytest.fixture
+def layer(monkeypatch):
+    """A Layer over a library that notes its calls, and refuses those whose name is in layer.refuse."""
+    one = object.__new__(b.Layer)
+    one.handle, one.dense, one.shared_selection, one.dims = None, False, False, (128, 2, 32, 4, 2)
+    one.workspace, one.dtype, one.batch, one.seq, one.seq_out = torch.empty(1), b.SH_F32, 2, 8, 8
+    one._settings, one._of_forward = {}, {}
+    one.calls, one.refuse = [], set()
+    for name in ("sh_set_qk_norm", "sh_set_balance", "sh_set_dropout", "sh_set_rope", "sh_forward", "sh_forward_timed", "sh_forward_stamped", "sh_backward"):
+        monkeypatch.setattr(b.lib, name, lambda *a, name=name: one.calls.append((name, a)) or (-1 if name in one.refuse else 0))
+    monkeypatch.setattr(b.lib, "sh_training_scratch_bytes", lambda *a: 64)
+    monkeypatch.setattr(b, "_stream", lambda: None)
+    return one
+
+
+@pytest.mark.parametrize("train", [True, False])
+def test_norms_that_are_off_have_no_gradients(layer, train):
+    gains = device_tensor(32), device_tensor(32)
+    layer.sh_set_qk_norm(*gains)
+    assert len(layer._settings["qk_norm"]) == 5
+    layer.sh_set_qk_norm(*gains, eps=0.0, train=train)
+    assert layer.calls[-1] == ("sh_set_qk_norm", (None, None, None, 0.0, None, None, None, 0))
+    x = device_tensor(2, 8, 128)
+    layer.sh_forward(x)
+    assert "qk_norm" not in layer._of_forward and set(layer.sh_backward(x, x)) == {"dx", "dWq", "dWk", "dWv", "dWo", "dWs", "dWd"}
+
+
+@pytest.mark.parametrize("eps", [1e-46, -1e-60, 5e-324])
+def test_an_eps_that_rounds_to_zero_is_refused(layer, eps):
+    layer.sh_set_qk_norm(device_tensor(32), None)
+    had, calls = dict(layer._settings), len(layer.calls)
+    with pytest.raises(ValueError, match="eps"):
+        layer.sh_set_qk_norm(device_tensor(32), None, eps=eps)
+    assert layer._settings == had and len(layer.calls) == calls
