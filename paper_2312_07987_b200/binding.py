@@ -258,15 +258,15 @@ class Layer:
         if out is None:
             out = torch.empty((x.shape[0], self.seq_out, x.shape[2]), dtype=getattr(self, "out_dtype", torch.float32), device=x.device)
         assert out.dtype == getattr(self, "out_dtype", torch.float32), "out must have the layer's output dtype (see sh_set_output_f16)"
-        self._of_forward = dict(self._settings)
         _check(lib.sh_forward(self.handle, _ptr(x), _ptr(out), _stream()))
+        self._of_forward = dict(self._settings)            # (a refused pass leaves the one before it, which keeps its tensors)
         return out
 
     def sh_forward_timed(self, x: torch.Tensor, out: torch.Tensor):
         """Returns the six stage times in ms: gate+sort, qk, v, attention, o, total."""
         ms = (ctypes.c_float * 6)()
-        self._of_forward = dict(self._settings)
         _check(lib.sh_forward_timed(self.handle, _ptr(x), _ptr(out), _stream(), ms))
+        self._of_forward = dict(self._settings)
         return list(ms)
 
     def sh_forward_stamped(self, x: torch.Tensor, out: torch.Tensor):
@@ -274,8 +274,8 @@ class Layer:
         nanoseconds of the device clock for the kernels that ran (see STAMP_KERNELS)."""
         n = len(STAMP_KERNELS)
         buf = (ctypes.c_uint64 * (3 * n))()
-        self._of_forward = dict(self._settings)
         _check(lib.sh_forward_stamped(self.handle, _ptr(x), _ptr(out), _stream(), buf))
+        self._of_forward = dict(self._settings)
         return {name: (buf[i], buf[n + i], buf[2 * n + i]) for i, name in enumerate(STAMP_KERNELS) if buf[2 * n + i] != 0}
 
     def sh_status_block(self):

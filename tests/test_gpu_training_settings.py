@@ -54,3 +54,27 @@ def test_norms_switched_off_with_their_gains():
     with pytest.raises(ValueError, match="eps"):
         layer.sh_set_qk_norm(*gains, eps=1e-46)
     layer.close()
+
+
+def test_a_refused_pass_leaves_the_one_before_it():
+    layer, x = tiny_layer()
+    G, D = torch.randn_like(x), layer.dims[2]
+    layer.sh_set_qk_norm(torch.rand(D, device="cuda"), None)
+    layer.sh_set_balance("entropy", 0.1)
+    layer.sh_set_dropout(0.3, torch.tensor([1, 2], device="cuda"))
+    layer.sh_forward(x)
+    want = layer.sh_backward(x, G)
+    layer.sh_set_qk_norm(None, torch.rand(D, device="cuda"))
+    layer.sh_set_balance("counts", 0.1)
+    layer.sh_set_dropout(0.6, torch.tensor([3, 4], device="cuda"))
+    off = torch.empty(x.numel() + 1, device="cuda")[1:].view(x.shape)
+    for call in (lambda: layer.sh_forward(off), lambda: layer.sh_forward(x, off), lambda: layer.sh_forward_timed(off, x), lambda: layer.sh_forward_stamped(off, x)):
+        with pytest.raises(binding.SwitchHeadError, match="aligned"):
+            call()
+    for n in range(4, 25):
+        torch.full((1 << n,), float("nan"), device="cuda")   # (what memory that nobody holds has in it)
+    got = layer.sh_backward(x, G)
+    assert set(got) == set(want) and "dgq" in got
+    for n, w in want.items():
+        assert float((got[n] - w).abs().max() / w.abs().max()) < 1e-4, n
+    layer.close()

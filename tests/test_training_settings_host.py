@@ -67,3 +67,25 @@ def test_an_eps_that_rounds_to_zero_is_refused(layer, eps):
     with pytest.raises(ValueError, match="eps"):
         layer.sh_set_qk_norm(device_tensor(32), None, eps=eps)
     assert layer._settings == had and len(layer.calls) == calls
+
+
+@pytest.mark.parametrize("name", ["sh_forward", "sh_forward_timed", "sh_forward_stamped"])
+def test_a_refused_pass_leaves_the_one_before_it(layer, name):
+    """Its tensors live on, and sh_backward's gradients of gains are its own."""
+    gq, x = device_tensor(32), device_tensor(2, 8, 128)
+    layer.sh_set_qk_norm(gq)
+    rng = device_tensor(2, dtype=torch.int64)
+    layer.sh_set_dropout(0.1, rng)
+    layer.sh_forward(x)
+    of_pass = dict(layer._settings)
+    assert layer._of_forward == of_pass
+    layer.sh_set_qk_norm(None, device_tensor(32))
+    layer.sh_set_dropout(0.5, device_tensor(2, dtype=torch.int64))
+    layer.refuse = {name}
+    with pytest.raises(b.SwitchHeadError):
+        getattr(layer, name)(x, x)
+    assert layer._of_forward is not layer._settings and all(layer._of_forward[n] is of_pass[n] for n in of_pass)
+    assert "dgq" in layer.sh_backward(x, x) and "dgk" not in layer.sh_backward(x, x)
+    layer.refuse = set()
+    getattr(layer, name)(x, x)
+    assert layer._of_forward == layer._settings and "dgk" in layer.sh_backward(x, x)
