@@ -729,7 +729,9 @@ extern "C" int sh_backward(sh_layer* L, const void* x, const float* dout, float*
   g_err[0] = 0;
   int rc = check_ready(L);
   if (rc != SH_OK) return rc;
-  if (L->dtype != SH_F32 || L->dense || L->d.sides != 2 || L->d.Tc > 0 || (L->rope && !L->fwd_train.norm.on) || L->xl_positions || L->moe_q || L->moe_k) {
+  // (a pass with a positional term of its own is not differentiable, see sh_forward; what has been switched on behind one that is does not matter)
+  const bool positional = !L->fwd_x && ((L->rope && !L->fwd_train.norm.on) || L->xl_positions);
+  if (L->dtype != SH_F32 || L->dense || L->d.sides != 2 || L->d.Tc > 0 || positional || L->moe_q || L->moe_k) {
     sh_set_error("sh_backward serves the fp32 configuration of the plain layer (two gates, dense Q/K, no cache, no positional term but "
                  "the rotation of normalised heads)");
     return SH_ERR_UNSUPPORTED;

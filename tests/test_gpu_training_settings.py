@@ -78,3 +78,47 @@ def test_a_refused_pass_leaves_the_one_before_it():
     for n, w in want.items():
         assert float((got[n] - w).abs().max() / w.abs().max()) < 1e-4, n
     layer.close()
+
+
+@pytest.mark.parametrize("later", ["rope", "rope and norms", "relative"])
+def test_positions_switched_on_between_the_passes(later):
+    """They are for the next forward pass: the one that was made had none, and is differentiated as it was."""
+    layer, x = tiny_layer()
+    G, (M, H, D, _, _) = torch.randn_like(x), layer.dims
+    layer.sh_forward(x)
+    want = layer.sh_backward(x, G)
+    plain = layer.sh_forward(x)
+    if later == "relative":
+        layer.sh_set_xl_positions(torch.randn(H, M, D, device="cuda"))
+    else:
+        layer.sh_set_rope(10000.0)
+        if later == "rope and norms":
+            layer.sh_set_qk_norm(torch.rand(D, device="cuda"), None)
+    got = layer.sh_backward(x, G)
+    assert set(got) == set(want)
+    for n, w in want.items():
+        assert float((got[n] - w).abs().max() / w.abs().max()) < 1e-4, n
+    assert not torch.equal(layer.sh_forward(x), plain)
+    if later == "rope and norms":
+        assert "dgq" in layer.sh_backward(x, G)
+    else:
+        with pytest.raises(binding.SwitchHeadError, match="UNSUPPORTED"):
+            layer.sh_backward(x, G)
+    layer.close()
+
+
+def test_rotation_of_norms_switched_on_behind_a_pass_without():
+    """Norms in both passes, the rotation in the second only: each is differentiated as it was made."""
+    layer, x = tiny_layer()
+    G = torch.randn_like(x)
+    layer.sh_set_qk_norm(torch.rand(layer.dims[2], device="cuda"), None)
+    layer.sh_forward(x)
+    want = layer.sh_backward(x, G)
+    layer.sh_set_rope(10000.0)
+    got = layer.sh_backward(x, G)
+    for n, w in want.items():
+        assert float((got[n] - w).abs().max() / w.abs().max()) < 1e-4, n
+    layer.sh_forward(x)
+    turned = layer.sh_backward(x, G)
+    assert float((turned["dWq"] - want["dWq"]).abs().max() / want["dWq"].abs().max()) > 1e-2
+    layer.close()
