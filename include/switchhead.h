@@ -395,8 +395,9 @@ size_t sh_training_scratch_bytes(const sh_layer* layer, int which);     /* 0: no
 int sh_set_qk_norm(sh_layer* layer, const float* gq, const float* gk, float eps, float* dgq, float* dgk, void* scratch, size_t scratch_bytes);
 
 /* sh_forward also gives the balance loss of its gates (of all tokens the layer sees, or those of mask [N]; one gate per head and
- * side): loss [1], counts and prob [sides, H, E] as sh_balance_loss.  sh_backward adds *gloss (NULL: 1) times its
- * gradient to those of the gates, so to dx, dWs and dWd.  loss = scratch = NULL switches it off. */
+ * side; behind a cache the destination side's of the chunk's tokens only, the ones it serves): loss [1], counts and prob [sides, H, E] as
+ * sh_balance_loss.  sh_backward adds *gloss (NULL: 1) times its gradient to those of the gates, so to dx, dWs and dWd.  loss = scratch = NULL
+ * switches it off. */
 int sh_set_balance(sh_layer* layer, int kind, float coef, const void* mask, float* loss, int32_t* counts, float* prob, const float* gloss,
                    void* scratch, size_t scratch_bytes);
 

@@ -226,7 +226,8 @@ class Layer:
 
     def sh_set_balance(self, kind: Optional[str], coef: float = 0.01, mask: Optional[torch.Tensor] = None, gloss: Optional[torch.Tensor] = None) -> Optional[dict]:
         """sh_forward also gives the balance loss of its gates (fp32 layers): returns the tensors it writes, {loss, counts, prob}; sh_backward
-        adds gloss times its gradient to the gates'.  kind: "counts", "entropy", or None to switch it off.  mask [batch * seq] bool: tokens that count."""
+        adds gloss times its gradient to the gates'.  kind: "counts", "entropy", or None to switch it off.  mask [batch * seq] bool: tokens that count (those of
+        a cache among them; the destination side's gates count the chunk's tokens only)."""
         if kind is None:
             _check(lib.sh_set_balance(self.handle, 0, 0.0, *([None] * 6), 0))
             self._settings.pop("balance", None)

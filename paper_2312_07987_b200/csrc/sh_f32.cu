@@ -295,17 +295,66 @@ sh_qk_norm_args norm_args(sh_layer* L, const ShQkNorm& n) {
   return a;
 }
 
-sh_balance_args balance_args(sh_layer* L, const ShBalance& b) {
+// With a cache and a gate of its own for each side the cached tokens have no destination side (no output row, no query): its gates' balance is
+// that of the chunk's tokens, the source side's of all.
+bool balance_apart(const ShDims& d) { return d.Tc > 0 && d.sides == 2; }
+// The scratch: logits [N, G], slope [G], the workspace; behind them, for two sides apart, which tokens the destination side counts and the two losses.
+struct BalanceScratch { size_t slope, workspace, mask, losses, total; };
+BalanceScratch balance_scratch(const ShDims& d) {
+  const bool two = balance_apart(d);
+  BalanceScratch s;
+  s.slope = up256((size_t)d.N * d.G * 4);
+  s.workspace = s.slope + up256((size_t)d.G * 4);
+  s.mask = s.workspace + up256(sh_balance_workspace_bytes(d.N, two ? 1 : d.sides, d.H, d.E));
+  s.losses = s.mask + (two ? up256((size_t)d.N) : 0);
+  s.total = s.losses + (two ? 256 : 0);
+  return s;
+}
+
+// All sides' gates, or those of one side.
+sh_balance_args balance_args(sh_layer* L, const ShBalance& b, int side = -1) {
   const ShDims& d = L->d;
+  const BalanceScratch s = balance_scratch(d);
+  const int first = side < 0 ? 0 : side;
+  const size_t cols = (size_t)first * d.H * d.E;           // of a token's logits, and of the results
   sh_balance_args a{};
-  a.n_tokens = d.N; a.token_stride = d.G; a.logits = b.scratch;
-  a.idx = (const int*)(L->ws + L->o.idx); a.mask = b.mask; a.gloss = b.gloss;
-  a.loss = b.loss; a.prob = b.prob; a.counts = b.counts;
-  const size_t logits = up256((size_t)d.N * d.G * 4), slope = up256((size_t)d.G * 4);
-  a.slope = (float*)(b.scratch + logits);
-  a.workspace = b.scratch + logits + slope; a.workspace_bytes = sh_balance_workspace_bytes(d.N, d.sides, d.H, d.E);
-  a.dtype = SH_F32; a.kind = b.kind; a.sides = d.sides; a.n_heads = d.H; a.n_experts = d.E; a.k = d.k; a.coef = b.coef;
+  a.n_tokens = d.N; a.token_stride = d.G; a.logits = (const float*)b.scratch + cols;
+  a.idx = (const int*)(L->ws + L->o.idx) + (size_t)first * d.N * d.H * d.k; a.mask = b.mask; a.gloss = b.gloss;
+  a.loss = b.loss; a.prob = b.prob + cols; a.counts = b.counts + cols;
+  a.slope = (float*)(b.scratch + s.slope) + cols;
+  a.workspace = b.scratch + s.workspace; a.workspace_bytes = s.mask - s.workspace;
+  a.dtype = SH_F32; a.kind = b.kind; a.sides = side < 0 ? d.sides : 1; a.n_heads = d.H; a.n_experts = d.E; a.k = d.k; a.coef = b.coef;
   return a;
+}
+
+__global__ void sh_f32_chunk_mask_kernel(const unsigned char* mask, unsigned char* out, ShDims d) {
+  pdl_wait();
+  for (int t = blockIdx.x * blockDim.x + threadIdx.x; t < d.N; t += gridDim.x * blockDim.x) out[t] = t % d.T >= d.Tc && (!mask || mask[t]);
+}
+__global__ void sh_f32_two_losses_kernel(const float* side, float* loss) {
+  pdl_wait();
+  *loss = side[0] + side[1];                               // (each rounded by itself)
+}
+
+int launch_balance_loss(sh_layer* L, const ShBalance& b, cudaStream_t st) {
+  const ShDims& d = L->d;
+  if (!balance_apart(d)) {
+    L->launches += sh_balance_workspace_bytes(d.N, d.sides, d.H, d.E) ? 2 : 1;
+    return sh_run_balance_loss(balance_args(L, b), chained(L), st);
+  }
+  const BalanceScratch s = balance_scratch(d);
+  unsigned char* mask = (unsigned char*)b.scratch + s.mask;
+  float* losses = (float*)(b.scratch + s.losses);
+  const int blocks = (d.N + 255) / 256;
+  if (int rc = launch_k(chained(L), sh_f32_chunk_mask_kernel, dim3((unsigned)(blocks < 4 * sm_count(L) ? blocks : 4 * sm_count(L))), dim3(256), 0, st, (const unsigned char*)b.mask, mask, d)) return rc;
+  for (int side = 0; side < 2; ++side) {
+    sh_balance_args a = balance_args(L, b, side);
+    a.loss = losses + side;
+    if (side) a.mask = mask;
+    if (int rc = sh_run_balance_loss(a, chained(L), st)) return rc;
+  }
+  L->launches += 2 + 2 * (sh_balance_workspace_bytes(d.N, 1, d.H, d.E) ? 2 : 1);
+  return launch_k(chained(L), sh_f32_two_losses_kernel, dim3(1), dim3(1), 0, st, (const float*)losses, b.loss);
 }
 
 sh_dropout_args dropout_args(sh_layer* L, const ShDropout& o, const void* x, void* y) {
@@ -382,10 +431,7 @@ int sh_f32_prepare(sh_layer* L) {
 }
 
 size_t sh_f32_norm_scratch(const sh_layer* L) { return up256(2 * raw_heads(L->d) * 4) + sh_qk_norm_workspace_bytes(L->d.Dt); }
-size_t sh_f32_balance_scratch(const sh_layer* L) {
-  const ShDims& d = L->d;
-  return up256((size_t)d.N * d.G * 4) + up256((size_t)d.G * 4) + sh_balance_workspace_bytes(d.N, d.sides, d.H, d.E);
-}
+size_t sh_f32_balance_scratch(const sh_layer* L) { return balance_scratch(L->d).total; }
 size_t sh_f32_dropout_scratch(const sh_layer* L) { return (size_t)sh_out_rows(L->d) * L->d.M * 4; }
 
 void sh_f32_release(sh_layer* L) {
@@ -427,10 +473,7 @@ int sh_f32_forward(sh_layer* L, const void* x, void* out, cudaStream_t st) {
   }
   sh_mark(L, 0, st);
   if ((rc = launch_gate_sort(L, x, v, nhd, st, tr.balance.on ? (float*)tr.balance.scratch : nullptr))) return rc;
-  if (tr.balance.on) {
-    if ((rc = sh_run_balance_loss(balance_args(L, tr.balance), chained(L), st))) return rc;
-    L->launches += sh_balance_workspace_bytes(d.N, d.sides, d.H, d.E) ? 2 : 1;
-  }
+  if (tr.balance.on && (rc = launch_balance_loss(L, tr.balance, st))) return rc;
   sh_mark(L, 1, st);
   if (L->ev && (rc = launch_x<X_QK>(L, st, qk))) return rc;
   if (L->moe_k) {

@@ -143,7 +143,7 @@ struct ShBalance {                     // sh_set_balance
   float *loss = nullptr, *prob = nullptr;
   int* counts = nullptr;
   const float* gloss = nullptr;
-  char* scratch = nullptr;             // logits [N, G], slope [G], workspace
+  char* scratch = nullptr;             // logits [N, G], slope [G], workspace (sh_f32.cu, BalanceScratch)
 };
 struct ShDropout {                     // sh_set_dropout
   bool on = false;

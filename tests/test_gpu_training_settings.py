@@ -1,5 +1,6 @@
 """Calls of the training operators and of the layer's training settings in combinations that their own tests do not make: inputs
 whose rows overlap, settings switched between the passes, refused calls, a cache, and sizes above the small kernels' limits."""
+import numpy as np
 import pytest
 import torch
 
@@ -121,4 +122,94 @@ def test_rotation_of_norms_switched_on_behind_a_pass_without():
     layer.sh_forward(x)
     turned = layer.sh_backward(x, G)
     assert float((turned["dWq"] - want["dWq"]).abs().max() / want["dWq"].abs().max()) > 1e-2
+    layer.close()
+
+
+def definition(z, idx, kind, coef, keep):
+    """Loss, counts and probabilities of one side's gates in fp64: z [N, H, E], idx [N, H, k], keep [N]."""
+    E, n = z.shape[2], int(keep.sum())
+    P = (torch.softmax(z, -1) * keep[:, None, None]).sum(0) / n
+    counts = ((idx.long()[..., None] == torch.arange(E, device=z.device)) & keep[:, None, None, None]).sum((0, 2))
+    f = counts.double() / counts.sum(-1, keepdim=True)
+    return coef * (E * (f * P).sum() if kind == "counts" else (P * torch.log(P)).sum()), counts, P
+
+
+def layer_logits(inp, x):
+    """The gates' logits [sides, N, H, E] in fp64, and how far the layer's fp32 sums over d_model may be from them."""
+    N, M = inp.x.shape[0] * inp.x.shape[1], inp.cfg.d_model
+    z, off = [], 0.0
+    for W, bias in ((inp.Ws, inp.bias_s), (inp.Wd, inp.bias_d)):
+        w, v = torch.from_numpy(np.asarray(W)).cuda().double(), x.view(N, M).double()
+        z.append(torch.einsum("nm,hme->nhe", v, w) + (0 if bias is None else torch.from_numpy(bias).cuda().double()))
+        off = max(off, float(torch.einsum("nm,hme->nhe", v.abs(), w.abs()).max()) * (M + 2) * U)
+    return torch.stack(z), off
+
+
+def check_statistics(got, want, kind, coef, z, off):
+    """want: definition() of each side.  p is off by the logits' error twice (numerator and sum) and 18 roundings and those of its exponent, P by as much
+    and 256 + N / 64 additions; the loss by that of its terms."""
+    sides, N, H, E = z.shape
+    assert torch.equal(got["counts"].long(), torch.stack([c for _, c, _ in want]))
+    P = torch.stack([p for _, _, p in want])
+    rel = 2 * off + (18 + 2 * float(z.abs().max()) + 256 + N / 64) * U
+    assert float(((got["prob"].double() - P) / P).abs().max()) < rel
+    scale = E if kind == "counts" else 1.0 + float(torch.log(P).abs().max())
+    assert abs(float(got["loss"]) - float(sum(l for l, _, _ in want))) < coef * sides * H * scale * (rel + 4 * U)
+
+
+@pytest.mark.parametrize("T,cache,B,H,E,k", [(60, 32, 2, 2, 4, 2), (40, 1, 3, 2, 5, 3), (33, 32, 2, 1, 8, 1), (1200, 500, 4, 8, 8, 2)])
+@pytest.mark.parametrize("kind,masked", [("counts", False), ("entropy", True)])
+def test_balance_behind_a_cache_counts_what_is_routed(T, cache, B, H, E, k, kind, masked):
+    """The destination side has no tokens of the cache: its gates' counts, means and loss are the chunk's."""
+    cfg = inputs.LayerConfig("cached", inputs.DTYPE_F32, B, T, 64, H, 32, E, k, seed=T)
+    inp = inputs.make_inputs(cfg)
+    layer = binding.layer_from_inputs(inp, cache_len=cache)
+    x = binding.to_device(inp.x, cfg.dtype)
+    plain = layer.sh_forward(x)
+    idx = layer.sh_gate_topk(x)[0]
+
+    def some():
+        m = torch.rand(B * T, device="cuda") < 0.6
+        m[T - 1::T] = True                                   # (a chunk is never without a token)
+        return m
+
+    mask = some() if masked else None
+    got = layer.sh_set_balance(kind, 0.1, mask)
+    chunk = (torch.arange(T, device="cuda") >= cache).repeat(B)
+    z, off = layer_logits(inp, x)
+
+    def check():
+        keep = torch.ones_like(chunk) if mask is None else mask
+        check_statistics(got, [definition(z[0], idx[0], kind, 0.1, keep), definition(z[1], idx[1], kind, 0.1, keep & chunk)], kind, 0.1, z, off)
+
+    y = layer.sh_forward(x)
+    check()
+    assert float((y - plain).abs().max()) < 1e-5 * float(plain.abs().max())
+    layer.sh_check_guards()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        layer.sh_forward(x, y)
+    for t in got.values():
+        t.zero_()
+    if mask is not None:
+        mask.copy_(some())                                   # (read by the pass, not before it)
+    graph.replay()
+    check()
+    assert layer.sh_last_status() == 0
+    layer.close()
+
+
+def test_balance_of_a_shared_gate_behind_a_cache_counts_all():
+    """One gate for both sides: its selections of the cached tokens serve their keys and values."""
+    cfg = inputs.LayerConfig("cached", inputs.DTYPE_F32, 2, 50, 64, 2, 32, 4, 2, seed=5)
+    inp = inputs.make_inputs(cfg)
+    layer = binding.layer_from_inputs(inp, shared_selection=True, cache_len=20)
+    x = binding.to_device(inp.x, cfg.dtype)
+    got = layer.sh_set_balance("counts", 0.1)
+    layer.sh_forward(x)
+    z, off = layer_logits(inp, x)
+    keep = torch.ones(100, dtype=torch.bool, device="cuda")
+    check_statistics(got, [definition(z[0], layer.sh_gate_topk(x)[0][0], "counts", 0.1, keep)], "counts", 0.1, z[:1], off)
     layer.close()
