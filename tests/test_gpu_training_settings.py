@@ -213,3 +213,56 @@ def test_balance_of_a_shared_gate_behind_a_cache_counts_all():
     keep = torch.ones(100, dtype=torch.bool, device="cuda")
     check_statistics(got, [definition(z[0], layer.sh_gate_topk(x)[0][0], "counts", 0.1, keep)], "counts", 0.1, z[:1], off)
     layer.close()
+
+
+@pytest.mark.parametrize("kind,masked", [("counts", False), ("entropy", True)])
+def test_balance_of_a_large_batch_in_the_layer(kind, masked):
+    """More than 4096 tokens and 2^18 logits: the sort in blocks of 128 tokens, sums and loss in two launches out of the layer's scratch, and what
+    sh_backward reads there; against the plain pass and the operators around it."""
+    cfg = inputs.LayerConfig("large", inputs.DTYPE_F32, 9, 500, 64, 4, 32, 16, 3, seed=11, zipf_bias=1.2)
+    N, H, E = 4500, 4, 16
+    assert binding.lib.sh_balance_workspace_bytes(N, 2, H, E) > 0
+    inp = inputs.make_inputs(cfg)
+    layer = binding.layer_from_inputs(inp)
+    x = binding.to_device(inp.x, cfg.dtype)
+    G = torch.randn_like(x)
+    mask = torch.rand(N, device="cuda") < 0.8 if masked else None
+    gloss = torch.full((), 3e4, device="cuda")               # (a gradient that shows beside the task's)
+    z, off = layer_logits(inp, x)
+    idx = layer.sh_gate_topk(x)[0]
+    zt = z.permute(1, 0, 2, 3).float().contiguous()
+    alone = binding.sh_balance_loss(zt, idx, kind=kind, coef=0.1, mask=mask)
+    dz = binding.sh_balance_backward(zt, alone["slope"], mask=mask, gloss=gloss)
+    plain = layer.sh_forward(x)
+    want = layer.sh_backward(x, G)
+    W = torch.stack([binding.to_device(w, cfg.dtype) for w in (inp.Ws, inp.Wd)])
+    d = dz.double()
+    share = dict(dx=torch.einsum("nshe,shme->nm", d, W.double()).view_as(x), dWs=torch.einsum("nm,nhe->hme", x.view(N, 64).double(), d[:, 0]),
+                 dWd=torch.einsum("nm,nhe->hme", x.view(N, 64).double(), d[:, 1]))
+    got = layer.sh_set_balance(kind, 0.1, mask, gloss)
+
+    def check(y, back):
+        keep = torch.ones(N, dtype=torch.bool, device="cuda") if mask is None else mask
+        check_statistics(got, [definition(z[s], idx[s], kind, 0.1, keep) for s in range(2)], kind, 0.1, z, off)
+        assert float((y - plain).abs().max()) < 1e-5 * float(plain.abs().max())
+        for n, w in want.items():
+            w = w.double() + share.get(n, 0.0)
+            assert float((back[n].double() - w).abs().max() / w.square().mean().sqrt()) < 2e-4, n
+            if n in share:                                   # (a loss that did not reach a gradient would be seen)
+                assert float(share[n].abs().max() / w.square().mean().sqrt()) > 1e-2, n
+
+    step = lambda: (layer.sh_forward(x), layer.sh_backward(x, G))
+    for _ in range(2):
+        check(*step())
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = step()
+    for t in (*got.values(), out[0], *out[1].values()):
+        t.fill_(7)
+    graph.replay()
+    check(*out)
+    assert layer.sh_last_status() == 0
+    layer.sh_check_guards()
+    layer.close()
