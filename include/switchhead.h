@@ -331,7 +331,8 @@ size_t sh_qk_norm_workspace_bytes(int d_head);
  *   SH_BALANCE_ENTROPY:  loss = coef * sum over the gates of  sum_e P_e ln P_e         (the negative entropy of the mean)
  * A negative entry of idx (or one that is no expert) is not counted.  A row of -inf only has p = 0.  No token that counts:
  * everything is zero.
- *   loss [1], prob, slope [sides, H, E] fp32, counts [sides, H, E] int32 (sums in 64 bits); slope = dloss/dprob / n, less its mean over the
+ *   loss [1], prob, slope [sides, H, E] fp32, counts [sides, H, E] int32 (p added in fp32 over 256 tokens at most, from there on in 64 bits,
+ *   rounded once for a block); slope = dloss/dprob / n, less its mean over the
  *   gate's experts (which changes no gradient), is what sh_balance_backward reads.
  * sh_balance_backward: dlogits = *gloss * dloss/dlogits (gloss: device, NULL: 1), in the type of the logits, tokens
  * dtoken_stride elements apart; the counts are constants of it.  Tokens that do not count get zeros.  Reads logits, mask,

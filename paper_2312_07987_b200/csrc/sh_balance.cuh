@@ -15,6 +15,9 @@
 #include "sh_vec.cuh"
 
 constexpr int BL_THREADS = 256, BL_BLOCKS = 3;     // (two rows a thread on their way, 24 warps an SM: 16 warps 5 % slower, more rows the same)
+// Rows of a thread whose p it adds in fp32 (a longer chain, of values of one sign, loses a bit with every doubling): more tokens are taken by
+// further launches, which add to the blocks' sums.  (Joined in shared memory inside the loop instead: 0.1 us more at 22 us.)
+constexpr int BL_CHAIN = 256;
 constexpr int BL_LOSS_THREADS = 512;
 constexpr int BL_MAX_BLOCKS = 512;         // blocks of the first kernel at most (rows of partial results)
 
@@ -29,6 +32,9 @@ struct BlArgs {
   float* part_p; int* part_n;              // [blocks][gates * E] sums of p; [blocks][gates * E] counts, then [blocks] tokens
   unsigned* ticket;                        // gates whose sums are done (set to zero by the first kernel)
 };
+
+// A launch of the sums of several: tokens of all of them (idx), and whether there is something to add to.
+struct BlPart { long long all; int add; };
 
 // Rows of a thread that are on their way together: 64 bytes of them.
 template <typename T, int W> struct BlAhead { static constexpr int N = W * (int)sizeof(T) >= 32 ? 2 : 4; };
@@ -93,10 +99,10 @@ __device__ __forceinline__ float bl_softmax(float2 (&f)[W / 2]) {
   return s == 0.f ? 0.f : __fdividef(1.f, s);
 }
 
-// A block's share of the sums, tokens tpb at a time from its place among `blocks` blocks on, gates g0 .. g0 + ng - 1: into s_p a row of
+// A block's share of the sums, tokens tpb at a time from its place among `blocks` blocks on (all: tokens of the call), gates g0 .. g0 + ng - 1: into s_p a row of
 // the block's sums of p, into s_n the counts (both cleared or overwritten here), into *s_tokens the tokens that count.
 template <typename T, int W, int L, bool VEC, int THREADS>
-__device__ __forceinline__ void bl_sums(const BlArgs& a, int block, int blocks, int g0, int ng, float (*s_p)[W * L + 1], int* s_n, int* s_tokens) {
+__device__ __forceinline__ void bl_sums(const BlArgs& a, long long all, int block, int blocks, int g0, int ng, float (*s_p)[W * L + 1], int* s_n, int* s_tokens) {
   constexpr int EP = W * L, AHEAD = BlAhead<T, W>::N, PICKS = 4 / L < 1 ? 1 : 4 / L;
   const int row = threadIdx.x / L, sub = threadIdx.x % L, at = sub * W;
   const int gl = row % a.per, tl = row / a.per, gate = g0 + gl;
@@ -112,7 +118,7 @@ __device__ __forceinline__ void bl_sums(const BlArgs& a, int block, int blocks, 
   const long long step = (long long)blocks * a.tpb;
   long long t = (long long)block * a.tpb + tl;           // (what is past the last token is not read)
   const T* z = (const T*)a.z + (long long)gate * a.E + at + t * a.zt;
-  const int* idx = a.idx + ((long long)(gate / a.H) * a.tokens * a.H + gate % a.H + t * a.H) * a.k;
+  const int* idx = a.idx + ((long long)(gate / a.H) * all * a.H + gate % a.H + t * a.H) * a.k;
   const long long zstep = step * a.zt, istep = step * a.H * a.k, rounds = (a.tokens - (long long)block * a.tpb + step - 1) / step;
   // (the next AHEAD rows are on their way while one is worked on)
   BlRow<T, W, VEC> rows[AHEAD];
@@ -172,7 +178,7 @@ __device__ __forceinline__ void bl_columns(const BlArgs& a, int ng, const float 
 }
 
 template <typename T, int W, int L, bool VEC>
-static __global__ void __launch_bounds__(BL_THREADS, BL_BLOCKS) sh_balance_sums_kernel(const BlArgs a) {
+static __global__ void __launch_bounds__(BL_THREADS, BL_BLOCKS) sh_balance_sums_kernel(const BlArgs a, const BlPart part) {
   constexpr int EP = W * L, ROWS = BL_THREADS / L;
   __shared__ float s_p[ROWS][EP + 1];
   __shared__ int s_n[ROWS * EP];                         // [gate of the block][expert]
@@ -182,13 +188,17 @@ static __global__ void __launch_bounds__(BL_THREADS, BL_BLOCKS) sh_balance_sums_
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.ticket = 0;
   const int g0 = blockIdx.y * a.per, ng = min(a.per, a.gates - g0);
-  bl_sums<T, W, L, VEC, BL_THREADS>(a, blockIdx.x, gridDim.x, g0, ng, s_p, s_n, &s_tokens);
+  bl_sums<T, W, L, VEC, BL_THREADS>(a, part.all, blockIdx.x, gridDim.x, g0, ng, s_p, s_n, &s_tokens);
   const long long base = (long long)blockIdx.x * a.gates * a.E + (long long)g0 * a.E;
   bl_columns<BL_THREADS, EP + 1>(a, ng, s_p, s_part, [&](int c, double sum) {
-    a.part_p[base + c] = (float)sum;                       // (hundreds of them, each rounded by itself)
-    a.part_n[base + c] = s_n[c / a.E * EP + c % a.E];
+    const int n = s_n[c / a.E * EP + c % a.E];
+    a.part_p[base + c] = (float)(part.add ? sum + a.part_p[base + c] : sum);      // (hundreds of them, each rounded by itself)
+    a.part_n[base + c] = part.add ? n + a.part_n[base + c] : n;
   });
-  if (blockIdx.y == 0 && threadIdx.x == 0) a.part_n[(long long)gridDim.x * a.gates * a.E + blockIdx.x] = s_tokens;
+  if (blockIdx.y == 0 && threadIdx.x == 0) {
+    int* tokens = a.part_n + (long long)gridDim.x * a.gates * a.E + blockIdx.x;
+    *tokens = part.add ? s_tokens + *tokens : s_tokens;
+  }
 }
 
 struct BlOut {
@@ -291,7 +301,7 @@ static __global__ void __launch_bounds__(BL_SMALL_THREADS, 1) sh_balance_small_k
   asm volatile("griddepcontrol.wait;" ::: "memory");
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank();
-  bl_sums<T, W, L, VEC, BL_SMALL_THREADS>(a, rank, BL_CLUSTER, 0, a.gates, s_p, s_n, &s_tokens);
+  bl_sums<T, W, L, VEC, BL_SMALL_THREADS>(a, a.tokens, rank, BL_CLUSTER, 0, a.gates, s_p, s_n, &s_tokens);
   bl_columns<BL_SMALL_THREADS, EP + 1>(a, a.gates, s_p, s_part, [&](int c, double sum) { s_sum[c] = sum; });
   cluster.sync();
   const int e = threadIdx.x & 31;

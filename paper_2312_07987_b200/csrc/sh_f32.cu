@@ -338,10 +338,7 @@ __global__ void sh_f32_two_losses_kernel(const float* side, float* loss) {
 
 int launch_balance_loss(sh_layer* L, const ShBalance& b, cudaStream_t st) {
   const ShDims& d = L->d;
-  if (!balance_apart(d)) {
-    L->launches += sh_balance_workspace_bytes(d.N, d.sides, d.H, d.E) ? 2 : 1;
-    return sh_run_balance_loss(balance_args(L, b), chained(L), st);
-  }
+  if (!balance_apart(d)) return sh_run_balance_loss(balance_args(L, b), chained(L), st, &L->launches);
   const BalanceScratch s = balance_scratch(d);
   unsigned char* mask = (unsigned char*)b.scratch + s.mask;
   float* losses = (float*)(b.scratch + s.losses);
@@ -351,9 +348,9 @@ int launch_balance_loss(sh_layer* L, const ShBalance& b, cudaStream_t st) {
     sh_balance_args a = balance_args(L, b, side);
     a.loss = losses + side;
     if (side) a.mask = mask;
-    if (int rc = sh_run_balance_loss(a, chained(L), st)) return rc;
+    if (int rc = sh_run_balance_loss(a, chained(L), st, &L->launches)) return rc;
   }
-  L->launches += 2 + 2 * (sh_balance_workspace_bytes(d.N, 1, d.H, d.E) ? 2 : 1);
+  L->launches += 2;
   return launch_k(chained(L), sh_f32_two_losses_kernel, dim3(1), dim3(1), 0, st, (const float*)losses, b.loss);
 }
 
@@ -582,8 +579,7 @@ int sh_f32_backward(sh_layer* L, const void* x, const float* dout, float* dx, fl
     a.norm.q_scale = 1.f;                                   // (the attention's gradient is that of the query before its scale)
     a.dgq = tr.norm.dgq; a.dgk = tr.norm.dgk;
     a.workspace = tr.norm.scratch + up256(2 * raw_heads(d) * 4); a.workspace_bytes = sh_qk_norm_workspace_bytes(d.Dt);
-    if ((rc = sh_run_qk_norm_backward(a, chained(L), st))) return rc;
-    more += a.dgq || a.dgk ? 2 : 1;
+    if ((rc = sh_run_qk_norm_backward(a, chained(L), st, &more))) return rc;
   }
   // value experts: their part of dx, and the source gates' gradients
   if ((rc = launch_d<X_DR>(L, st, src))) return rc;

@@ -267,10 +267,11 @@ bool sh_bf16_gate_ok(const sh_layer* L);        // its logits fit shared memory 
 // The CUDA-core attention kernel on fp32 storage (the relative-position term of Transformer-XL).
 int sh_simt_attention_f32(sh_layer* L, cudaStream_t st);
 
-// The operators of a training step (sh_train.cu): checks of the arguments and launches; pdl: chained to the kernel before.
+// The operators of a training step (sh_train.cu): checks of the arguments and launches; pdl: chained to the kernel before; launches: where their
+// number is added.
 int sh_run_qk_norm(const sh_qk_norm_args& p, bool pdl, cudaStream_t st);
-int sh_run_qk_norm_backward(const sh_qk_norm_backward_args& p, bool pdl, cudaStream_t st);
-int sh_run_balance_loss(const sh_balance_args& p, bool pdl, cudaStream_t st);
+int sh_run_qk_norm_backward(const sh_qk_norm_backward_args& p, bool pdl, cudaStream_t st, int* launches = nullptr);
+int sh_run_balance_loss(const sh_balance_args& p, bool pdl, cudaStream_t st, int* launches = nullptr);
 int sh_run_balance_backward(const sh_balance_args& p, bool add, bool pdl, cudaStream_t st);   // add: dlogits += (fp32)
 int sh_run_dropout(const sh_dropout_args& p, bool pdl, cudaStream_t st);
 

@@ -162,7 +162,7 @@ int qn_dispatch(const QnArgs& a, int v, int lanes, bool halves, bool backward, b
   return a.R ? qn_lanes_of<T, 1, true>(a, lanes, backward, pdl, blocks, st) : qn_lanes_of<T, 1, false>(a, lanes, backward, pdl, blocks, st);
 }
 
-int qn_run(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, bool pdl, cudaStream_t st) {
+int qn_run(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, bool pdl, cudaStream_t st, int* launches = nullptr) {
   const bool backward = back != nullptr;
   int sms = 0;
   if (int rc = device_sms(&sms)) return rc;
@@ -202,8 +202,10 @@ int qn_run(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, bool 
            : p.dtype == SH_BF16 ? qn_dispatch<__nv_bfloat16>(a, v, lanes, halves, backward, pdl, (int)blocks, st)
                                 : qn_dispatch<__half>(a, v, lanes, halves, backward, pdl, (int)blocks, st);
     if (rc) return rc;
+    if (launches) ++*launches;
   }
   if (backward && (back->dgq || back->dgk)) {
+    if (launches) ++*launches;
     QnGain g{a.part, {back->dgq, back->dgk}, {0, a.blocks0, (int)blocks}, p.d_head};
     return launch_k(blocks > 0, sh_qk_norm_gain_kernel, dim3((unsigned)((p.d_head + 31) / 32), 2), dim3(32, 32), 0, st, g);
   }
@@ -289,7 +291,7 @@ void bl_fill(const sh_balance_args& p, const BlPlan& pl, BlArgs& a) {
 }
 
 template <typename T, int W, int L, bool VEC>
-int bl_launch(const BlArgs& a, const BlPlan& p, int what, const BlOut* o, bool pdl, cudaStream_t st) {
+int bl_launch(const BlArgs& a, const BlPlan& p, int what, const BlOut* o, const BlPart& part, bool pdl, cudaStream_t st) {
   const dim3 grid((unsigned)p.nx, (unsigned)p.ny);
   if (what == 0 && o) {
     cudaLaunchConfig_t cfg = {};
@@ -303,15 +305,15 @@ int bl_launch(const BlArgs& a, const BlPlan& p, int what, const BlOut* o, bool p
     SH_CUDA_CHECK(cudaLaunchKernelEx(&cfg, sh_balance_small_kernel<T, W, L, VEC>, a, *o));
     return SH_OK;
   }
-  if (what == 0) return launch_k(pdl, sh_balance_sums_kernel<T, W, L, VEC>, grid, dim3(BL_THREADS), 0, st, a);
+  if (what == 0) return launch_k(pdl, sh_balance_sums_kernel<T, W, L, VEC>, grid, dim3(BL_THREADS), 0, st, a, part);
   if constexpr (sizeof(T) == 4)
     if (what == 2) return launch_k(pdl, sh_balance_backward_kernel<T, W, L, VEC, true>, grid, dim3(BL_THREADS), 0, st, a);
   return launch_k(pdl, sh_balance_backward_kernel<T, W, L, VEC, false>, grid, dim3(BL_THREADS), 0, st, a);
 }
 
 // what: 0 the sums (with `o`: and the loss), 1 dz, 2 dz added (fp32)
-int bl_dispatch(int dtype, const BlArgs& a, const BlPlan& p, int what, const BlOut* o, bool pdl, cudaStream_t st) {
-#define SH_BL(T, W, L) return p.vec ? bl_launch<T, W, L, true>(a, p, what, o, pdl, st) : bl_launch<T, W, L, false>(a, p, what, o, pdl, st)
+int bl_dispatch(int dtype, const BlArgs& a, const BlPlan& p, int what, const BlOut* o, const BlPart& part, bool pdl, cudaStream_t st) {
+#define SH_BL(T, W, L) return p.vec ? bl_launch<T, W, L, true>(a, p, what, o, part, pdl, st) : bl_launch<T, W, L, false>(a, p, what, o, part, pdl, st)
   if (dtype == SH_F32) {
     if (p.w == 4) SH_BL(float, 4, 1);
     if (p.l == 1) SH_BL(float, 8, 1);
@@ -340,17 +342,17 @@ int sh_run_qk_norm(const sh_qk_norm_args& p, bool pdl, cudaStream_t st) {
   return qn_run(p, nullptr, pdl, st);
 }
 
-int sh_run_qk_norm_backward(const sh_qk_norm_backward_args& p, bool pdl, cudaStream_t st) {
+int sh_run_qk_norm_backward(const sh_qk_norm_backward_args& p, bool pdl, cudaStream_t st, int* launches) {
   if (int rc = qn_check(p.norm, &p)) return rc;
   if (p.dgq || p.dgk) {
     const size_t need = sh_qk_norm_workspace_bytes(p.norm.d_head);
     if (!p.workspace || (uintptr_t)p.workspace % 256) { sh_set_error("workspace must be a device pointer aligned to 256 bytes"); return SH_ERR_WORKSPACE; }
     if (p.workspace_bytes < need) { sh_set_error("workspace too small: %zu bytes given, %zu needed", p.workspace_bytes, need); return SH_ERR_WORKSPACE; }
   }
-  return qn_run(p.norm, &p, pdl, st);
+  return qn_run(p.norm, &p, pdl, st, launches);
 }
 
-int sh_run_balance_loss(const sh_balance_args& p, bool pdl, cudaStream_t st) {
+int sh_run_balance_loss(const sh_balance_args& p, bool pdl, cudaStream_t st, int* launches) {
   if (int rc = bl_check(p, false)) return rc;
   int sms = 0;
   if (int rc = device_sms(&sms)) return rc;
@@ -361,12 +363,21 @@ int sh_run_balance_loss(const sh_balance_args& p, bool pdl, cudaStream_t st) {
   BlOut o{};
   o.gates = a.gates; o.E = a.E; o.kind = p.kind; o.coef = p.coef;
   o.loss = p.loss; o.prob = p.prob; o.slope = p.slope; o.counts = p.counts;
-  if (small) return bl_dispatch(p.dtype, a, pl, 0, &o, pdl, st);
+  if (launches) ++*launches;                               // (the last one)
+  if (small) return bl_dispatch(p.dtype, a, pl, 0, &o, BlPart{}, pdl, st);
   char* ws = (char*)p.workspace;
   a.ticket = (unsigned*)ws;
   a.part_p = (float*)(ws + kBlHead + bl_losses(a.gates));
   a.part_n = (int*)(a.part_p + (size_t)pl.nx * a.gates * a.E);
-  if (int rc = bl_dispatch(p.dtype, a, pl, 0, nullptr, pdl, st)) return rc;
+  const long long most = (long long)BL_CHAIN * pl.nx * pl.tpb;                // tokens of a launch
+  for (long long t = 0; t == 0 || t < p.n_tokens; t += most) {
+    a.z = (const char*)p.logits + t * p.token_stride * (long long)elem_bytes(p.dtype);
+    a.idx = p.idx + t * p.n_heads * p.k;
+    a.mask = p.mask ? (const unsigned char*)p.mask + t : nullptr;
+    a.tokens = p.n_tokens - t < most ? p.n_tokens - t : most;
+    if (int rc = bl_dispatch(p.dtype, a, pl, 0, nullptr, BlPart{p.n_tokens, t > 0}, pdl || t > 0, st)) return rc;
+    if (launches) ++*launches;
+  }
   o.part_p = a.part_p; o.part_n = a.part_n; o.ticket = a.ticket; o.gate_loss = (double*)(ws + kBlHead);
   o.blocks = pl.nx;
   return launch_k(true, sh_balance_loss_kernel, dim3((unsigned)a.gates), dim3(BL_LOSS_THREADS), 0, st, o);
@@ -380,7 +391,7 @@ int sh_run_balance_backward(const sh_balance_args& p, bool add, bool pdl, cudaSt
   const BlPlan pl = bl_plan_for(p, true, false, sms);
   BlArgs a;
   bl_fill(p, pl, a);
-  return bl_dispatch(p.dtype, a, pl, add ? 2 : 1, nullptr, pdl, st);
+  return bl_dispatch(p.dtype, a, pl, add ? 2 : 1, nullptr, BlPart{}, pdl, st);
 }
 
 int sh_run_dropout(const sh_dropout_args& p, bool pdl, cudaStream_t st) {

@@ -266,3 +266,46 @@ def test_balance_of_a_large_batch_in_the_layer(kind, masked):
     assert layer.sh_last_status() == 0
     layer.sh_check_guards()
     layer.close()
+
+
+def test_balance_of_tokens_that_share_their_logits():
+    """The mean of one row's p over 2^28 tokens is p: a thread adds 256 of them in 32 bits, a launch of the sums is rounded once."""
+    N = (1 << 28) + 12345
+    g = torch.Generator(device="cuda").manual_seed(4)
+    row = torch.randn(1, 1, 1, 4, generator=g, device="cuda")
+    idx = torch.randint(-1, 5, (1, N, 1, 1), generator=g, device="cuda", dtype=torch.int32)
+    mask = torch.rand(N, generator=g, device="cuda") < 0.9
+    got = binding.sh_balance_loss(row.expand(N, 1, 1, 4), idx, mask=mask)
+    counts = torch.stack([((idx.view(-1) == e) & mask).sum() for e in range(4)])
+    assert torch.equal(got["counts"].view(4).long(), counts)
+    p = torch.softmax(row.double(), -1).view(4)
+    off = float(((got["prob"].view(4).double() - p) / p).abs().max())
+    assert off < (18 + 2 * float(row.abs().max()) + 256 + 12) * U, off
+    del idx, mask
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("S,H,E,ty", [(2, 4, 32, torch.bfloat16), (1, 3, 20, torch.float32)])
+def test_balance_sums_of_several_launches(S, H, E, ty):
+    """Tokens of their own logits, selections and mask, more than one launch of the sums takes: every token counts once."""
+    N, chunk = 6000007, 500000
+    g = torch.Generator(device="cuda").manual_seed(E)
+    z = torch.empty(N, S, H, E, dtype=ty, device="cuda").normal_(generator=g)
+    idx = torch.randint(-1, E, (S, N, H, 2), generator=g, device="cuda", dtype=torch.int32)
+    mask = torch.rand(N, generator=g, device="cuda") < 0.5
+    got, again = (binding.sh_balance_loss(z, idx, kind="entropy", mask=mask) for _ in range(2))
+    assert all(torch.equal(got[n], again[n]) for n in got)
+    P, counts = torch.zeros(S, H, E, dtype=torch.float64, device="cuda"), torch.zeros(S, H, E, dtype=torch.int64, device="cuda")
+    for t in range(0, N, chunk):
+        m = mask[t:t + chunk]
+        P += (torch.softmax(z[t:t + chunk].double(), -1) * m[:, None, None, None]).sum(0)
+        picks = torch.where(m[None, :, None, None], idx[:, t:t + chunk], -1).permute(0, 2, 1, 3).reshape(S, H, -1)
+        counts += torch.stack([(picks == e).sum(-1) for e in range(E)], -1)
+    P /= mask.sum()
+    assert torch.equal(got["counts"].long(), counts)
+    off = (18 + 2 * float(z.abs().max()) + 256 + 8) * U
+    assert float(((got["prob"].double() - P) / P).abs().max()) < off
+    loss = float((P * torch.log(P)).sum())
+    assert abs(float(got["loss"]) - loss) < S * H * (1 + float(torch.log(P).abs().max())) * off
+    del z, idx
+    torch.cuda.empty_cache()
