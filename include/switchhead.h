@@ -289,7 +289,7 @@ typedef struct {
  *   n = g o x / sqrt(mean(x^2) + eps),   y = Rot(position) n   (queries: times q_scale)
  * Rot turns the pair i < rotated/2 of the first `rotated` columns by position * base^(-2i/rotated): the columns (2i, 2i+1), as
  * sh_set_rope does, or with halves != 0 the columns (i, i + rotated/2).  rotated = 0: no rotation.  Statistics in fp32, one rounding to
- * the stored type.  Angles are good to 2^-24 turns at every position a 32-bit integer holds (16-bit types: and sine and cosine
+ * the stored type.  Angles are good to 2^-24 turns at every position a 32-bit integer holds for a base of at least 1 (16-bit types: and sine and cosine
  * to 2^-21).
  *   dtype      of q, k, their outputs and gradients: SH_F32, SH_BF16 or SH_F16
  *   q, k       q_heads, k_heads may be 0 (that side is left out), and need not be equal (grouped heads)
@@ -310,8 +310,8 @@ typedef struct {
 int sh_qk_norm(const sh_qk_norm_args* args, void* stream);
 
 /* Its gradients: norm.q, norm.k are the inputs of the forward call, dq, dk the gradients of its outputs.  Writes the gradients
- * of q and k to norm.q_out, norm.k_out and those of the gains, summed over tokens and heads, to dgq, dgk [d_head] fp32 (NULL: not
- * wanted; a sum over no rows is zero).  The workspace, sh_qk_norm_workspace_bytes(d_head) bytes aligned to 256, is wanted with
+ * of q and k to norm.q_out, norm.k_out and those of the gains, summed over tokens and heads (in fp32 over 512 rows and a block, in 64
+ * bits over the blocks), to dgq, dgk [d_head] fp32 (NULL: not wanted; a sum over no rows is zero).  The workspace, sh_qk_norm_workspace_bytes(d_head) bytes aligned to 256, is wanted with
  * dgq or dgk.  The same inputs give the same bits. */
 typedef struct {
   sh_qk_norm_args norm;

@@ -114,7 +114,8 @@ void qn_fill(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, QnA
   a.tokens = (long long)p.batch * p.seq;
   a.eps = p.eps;
   a.blocks0 = 0; a.part = nullptr;
-  // (frequencies by one multiplication each: 64 bits of mantissa, off by a few units of 2^-63 relative at the last)
+  // (frequencies by one multiplication each, 64 bits of mantissa: the roundings and the ratio's own add up, base >= 1, to less than 4 units of 2^-64
+  //  turns at any pair - 62 relative at the last of 128 -, with the cut to 64 bits 2^-30 turns at position 2^31)
   if (p.rotated) {
     const long double two_pi = 6.283185307179586476925286766559005768L, ratio = powl((long double)p.base, -2.0L / p.rotated);
     long double f = 1.0L / two_pi;
@@ -181,7 +182,7 @@ int qn_run(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, bool 
   for (int i = 0; i < 2; ++i) a.s[i].chunks = qn_divisor((unsigned)c[i]);
   a.chunks = qn_divisor((unsigned)(c[0] + c[1]));
   a.large = items[0] + items[1] > (1ll << 31) - (1 << 24);   // (a grid's last round goes past the end)
-  long long blocks = (items[0] + items[1] + groups - 1) / groups;
+  long long blocks = (items[0] + items[1] + groups - 1) / groups, step[2] = {0, 0}, many = 1;
   if (backward) {
     long long n[2];
     for (int i = 0; i < 2; ++i) n[i] = (items[i] + groups - 1) / groups;
@@ -195,12 +196,22 @@ int qn_run(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, bool 
     a.blocks0 = (int)n[0];
     blocks = n[0] + n[1];
     a.part = (float*)back->workspace;
+    for (int i = 0; i < 2; ++i) step[i] = n[i] * groups;
+    many = back->dgq || back->dgk ? QN_CHAIN / a.per : items[0] + items[1];
   }
   if (blocks > 0x7fffffffll) { sh_set_error("too many rows: batch * seq * heads / %d must be below 2^31", groups); return SH_ERR_UNSUPPORTED; }
-  if (blocks) {
-    int rc = p.dtype == SH_F32 ? qn_dispatch<float>(a, v, lanes, halves, backward, pdl, (int)blocks, st)
-           : p.dtype == SH_BF16 ? qn_dispatch<__nv_bfloat16>(a, v, lanes, halves, backward, pdl, (int)blocks, st)
-                                : qn_dispatch<__half>(a, v, lanes, halves, backward, pdl, (int)blocks, st);
+  // (backward, with gains: `many` rounds of the grid to a launch, QN_CHAIN rows of a thread)
+  bool more = blocks > 0;
+  for (long long r = 0; more; r += many) {
+    more = false;
+    for (int i = 0; i < 2; ++i) {
+      a.s[i].from = r * step[i]; a.s[i].to = items[i];
+      if (backward && (items[i] - a.s[i].from + step[i] - 1) / (step[i] ? step[i] : 1) > many) { a.s[i].to = a.s[i].from + many * step[i]; more = true; }
+    }
+    const bool chain = pdl || r > 0;
+    int rc = p.dtype == SH_F32 ? qn_dispatch<float>(a, v, lanes, halves, backward, chain, (int)blocks, st)
+           : p.dtype == SH_BF16 ? qn_dispatch<__nv_bfloat16>(a, v, lanes, halves, backward, chain, (int)blocks, st)
+                                : qn_dispatch<__half>(a, v, lanes, halves, backward, chain, (int)blocks, st);
     if (rc) return rc;
     if (launches) ++*launches;
   }

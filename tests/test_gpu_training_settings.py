@@ -268,6 +268,32 @@ def test_balance_of_a_large_batch_in_the_layer(kind, masked):
     layer.close()
 
 
+@pytest.mark.parametrize("heads", [(1, 0), (12, 1), (3, 8)])
+def test_gain_gradients_of_many_rows(heads):
+    """Sums of one sign over hundreds of millions of rows (one row that all share): what a row gives times their number.  A thread's fp32 sum is of 512
+    rows, joined in 32 bits over 32 groups of a block and the launches, beyond the blocks in 64."""
+    B, T = 32, (1 << 27) // (32 * sum(heads)) + 3
+    g = torch.Generator(device="cuda").manual_seed(3)
+    row, drow = (torch.rand(1, 1, 1, 2, generator=g, device="cuda") + 0.3 for _ in range(2))
+    gain = torch.tensor([0.7, 1.3], device="cuda")
+    q, dq = (t.expand(B, T, heads[0], 2) for t in (row, drow))
+    k, dk = (t.expand(B, T, heads[1], 2) if heads[1] else None for t in (row, drow))
+    outs = []
+    for _ in range(2):
+        back = binding.sh_qk_norm_backward(q, k, dq, dk, gain, gain if heads[1] else None)
+        one = binding.sh_qk_norm_backward(row, None, drow, None, gain)
+        outs.append([back["dgq"]] + ([back["dgk"]] if heads[1] else []))
+        assert all((back[n] == one["dq"]).all() for n in ("dq", "dk") if back[n] is not None)
+        del back
+    share = row.double() * drow.double() / torch.sqrt(row.double().square().mean(-1, keepdim=True) + 1e-6)
+    # (a row's share: the sum of squares, root, two products: 10 U; 37 launches at most)
+    for dg, n in zip(outs[0], heads):
+        want = share.view(2) * (B * T * n)
+        assert float(((dg.double() - want) / want).abs().max()) < (10 + 512 + 32 + 40) * U, (dg, want)
+    assert all(torch.equal(a, c) for a, c in zip(*outs))
+    torch.cuda.empty_cache()
+
+
 def test_balance_of_tokens_that_share_their_logits():
     """The mean of one row's p over 2^28 tokens is p: a thread adds 256 of them in 32 bits, a launch of the sums is rounded once."""
     N = (1 << 28) + 12345
