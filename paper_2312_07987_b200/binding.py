@@ -378,7 +378,9 @@ _DTYPES = {torch.float32: SH_F32, torch.bfloat16: SH_BF16, torch.float16: SH_F16
 _NO_HEADS = (0, 0, 0, 0)
 
 
-_current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream    # (torch.cuda's own make objects first: 2 us of a 10 us call)
+# (torch.cuda's own make objects first: 2 us of a 10 us call; they serve where a torch has not these names, which are not public)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 def _launch(fn, packed: bytes, device: int) -> None:

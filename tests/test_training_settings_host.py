@@ -1,4 +1,8 @@
 """What the binding does around the training operators and the layer's training settings, without a GPU."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -89,3 +93,41 @@ def test_a_refused_pass_leaves_the_one_before_it(layer, name):
     layer.refuse = set()
     getattr(layer, name)(x, x)
     assert layer._of_forward == layer._settings and "dgk" in layer.sh_backward(x, x)
+
+
+WITHOUT = """
+import torch
+for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"):
+    if hasattr(torch._C, name):
+        delattr(torch._C, name)
+from paper_2312_07987_b200 import binding as b
+assert b._current_device is torch.cuda.current_device
+"""
+
+
+def run_without_private_names(more=""):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run([sys.executable, "-c", WITHOUT + more], check=True, cwd=root, timeout=300)
+
+
+def test_the_binding_needs_no_private_names_of_torch():
+    run_without_private_names("""
+class Stream:
+    cuda_stream = 77
+torch.cuda.current_stream = lambda device: Stream if device == 3 else None
+assert b._raw_stream(3) == 77
+""")
+
+
+@pytest.mark.gpu
+def test_calls_without_private_names_of_torch():
+    run_without_private_names("""
+x, rng = torch.ones(64, 64, device="cuda"), torch.tensor([1, 2], device="cuda")
+side = torch.cuda.Stream()
+side.wait_stream(torch.cuda.current_stream())
+with torch.cuda.stream(side):
+    assert b._raw_stream(0) == side.cuda_stream
+    y = b.sh_dropout(x, rng, 0.5)
+side.synchronize()
+assert torch.equal(y, b.sh_dropout(x, rng, 0.5)) and set(y.unique().tolist()) == {0.0, 2.0}
+""")
