@@ -45,10 +45,13 @@ int pow2_at_least(int n) { int p = 1; while (p < n) p *= 2; return p; }
 
 // ---- norms of queries and keys ----
 
-// Two elements of an output at one address: a dimension of more than one has no stride.
-bool apart(const char* what, std::initializer_list<std::pair<long long, long long>> dims) {
+// Two elements of an output at one address: its rows of `width` values are not as far apart in a dimension of more than one.
+bool apart(const char* what, long long width, std::initializer_list<std::pair<long long, long long>> dims) {
   for (auto& d : dims)
-    if (d.first > 1 && d.second == 0) { sh_set_error("%s: elements of an output must not share an address (stride 0)", what); return false; }
+    if (d.first > 1 && d.second < width && d.second > -width) {
+      sh_set_error("%s: elements of an output must not share an address (rows of %lld values, a stride of %lld)", what, width, d.second);
+      return false;
+    }
   return true;
 }
 
@@ -92,7 +95,7 @@ int qn_check(const sh_qk_norm_args& a, const sh_qk_norm_backward_args* back) {
     if (!s.x.data || !s.y.data) { sh_set_error("%s and %s must not be NULL", s.in, s.out); return SH_ERR_INVALID_ARG; }
     if (s.dy && !s.dy->data) { sh_set_error("d%s must not be NULL", s.in); return SH_ERR_INVALID_ARG; }
     if (!aligned_to(elem_bytes(a.dtype), "q, k, their outputs and gradients", {s.x.data, s.y.data, s.dy ? s.dy->data : nullptr})) return SH_ERR_INVALID_ARG;
-    if (!apart(s.out, {{a.batch, s.y.batch_stride}, {a.seq, s.y.token_stride}, {s.heads, s.y.head_stride}})) return SH_ERR_INVALID_ARG;
+    if (!apart(s.out, a.d_head, {{a.batch, s.y.batch_stride}, {a.seq, s.y.token_stride}, {s.heads, s.y.head_stride}})) return SH_ERR_INVALID_ARG;
   }
   return SH_OK;
 }
@@ -278,7 +281,7 @@ int bl_check(const sh_balance_args& a, bool backward) {
   if (!aligned_to(4, "idx, loss, prob, slope, counts and gloss", {a.idx, a.loss, a.prob, a.slope, a.counts, a.gloss})) return SH_ERR_INVALID_ARG;
   if (backward) {
     if (!a.slope || (a.n_tokens && !a.dlogits)) { sh_set_error("slope and dlogits must not be NULL"); return SH_ERR_INVALID_ARG; }
-    return apart("dlogits", {{a.n_tokens, a.dtoken_stride}}) ? SH_OK : SH_ERR_INVALID_ARG;
+    return apart("dlogits", gates * a.n_experts, {{a.n_tokens, a.dtoken_stride}}) ? SH_OK : SH_ERR_INVALID_ARG;
   }
   if (a.k < 1 || a.k > a.n_experts) { sh_set_error("k must be in 1..n_experts (got k=%d, n_experts=%d)", a.k, a.n_experts); return SH_ERR_INVALID_ARG; }
   if (a.n_tokens >= (1ll << 31) / a.k) { sh_set_error("n_tokens * k must be below 2^31 (got %lld, %d)", (long long)a.n_tokens, a.k); return SH_ERR_UNSUPPORTED; }
@@ -414,7 +417,7 @@ int sh_run_dropout(const sh_dropout_args& p, bool pdl, cudaStream_t st) {
   }
   if (!(p.p >= 0.0 && p.p <= 1.0)) { sh_set_error("p must be in 0..1 (got %g)", p.p); return SH_ERR_INVALID_ARG; }
   if (p.rows == 0 || p.cols == 0) return SH_OK;
-  if (!apart("y", {{p.rows, p.y_stride}})) return SH_ERR_INVALID_ARG;
+  if (!apart("y", p.cols, {{p.rows, p.y_stride}})) return SH_ERR_INVALID_ARG;
   if (!p.x || !p.y || !p.rng) { sh_set_error("x, y and rng must not be NULL"); return SH_ERR_INVALID_ARG; }
   if (!aligned_to(8, "rng", {p.rng}) || !aligned_to(elem_bytes(p.dtype), "x, residual and y", {p.x, p.residual, p.y})) return SH_ERR_INVALID_ARG;
   int sms = 0;

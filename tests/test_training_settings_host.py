@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from paper_2312_07987_b200 import binding as b
+from tests import test_training_operators_host as given
 
 
 @pytest.mark.parametrize("shape,strides", [((2, 3, 2, 8), (100, 1, 40, 1)), ((3, 4, 2, 16), (4, 12, 1, 1)), ((2, 3, 2, 8), (0, 1, 0, 1)), ((2, 3, 2, 8), (1, 1, 1, 1)),
@@ -131,3 +132,24 @@ with torch.cuda.stream(side):
 side.synchronize()
 assert torch.equal(y, b.sh_dropout(x, rng, 0.5)) and set(y.unique().tolist()) == {0.0, 2.0}
 """)
+
+
+@pytest.mark.parametrize("stride", [1, 31, -31])
+@pytest.mark.parametrize("which", ["batch_stride", "token_stride", "head_stride"])
+def test_heads_of_an_output_that_overlap_are_refused(which, stride):
+    for fn, backward in ((b.lib.sh_qk_norm, False), (b.lib.sh_qk_norm_backward, True)):
+        for out in ("q_out", "k_out"):
+            assert fn(given.norm_args({out: {which: stride}}, backward), None) == -1 and "share an address" in b.sh_last_error()
+    # (a dimension of one has no stride)
+    size = dict(batch_stride=dict(batch=1), token_stride=dict(seq=1), head_stride=dict(q_heads=1, k_heads=1))[which]
+    fn = b.lib.sh_qk_norm
+    assert fn(given.norm_args(dict(q_out={which: stride}, k=dict(data=0)), **size), None) == -1 and "k and k_out" in b.sh_last_error()
+
+
+def test_other_outputs_that_overlap_are_refused():
+    for stride in (15, 1, -15):                              # sides * heads * experts = 16
+        assert b.lib.sh_balance_backward(given.balance_args(dtoken_stride=stride), None) == -1 and "share an address" in b.sh_last_error()
+    f = dict(x=given.PTR, residual=0, y=given.PTR, rng=given.PTR, rows=4, cols=64, x_stride=64, residual_stride=64, y_stride=63, p=0.1, dtype=b.SH_F32, reserved=0)
+    for stride in (63, 1, -63):
+        f["y_stride"] = stride
+        assert b.lib.sh_dropout(b._DROPOUT.pack(*[f[n] for n in given.DROPOUT]), None) == -1 and "share an address" in b.sh_last_error()
