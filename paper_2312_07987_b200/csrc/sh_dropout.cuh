@@ -209,7 +209,7 @@ static __global__ void __launch_bounds__(DO_THREADS) sh_dropout_flat_kernel(cons
 // the other, and its pieces go through shared memory.  16384 x 2001 in bf16: 73 us; with each lane's values straight from memory 91.
 template <typename T, bool RES>
 static __global__ void __launch_bounds__(DO_THREADS) sh_dropout_rows_kernel(const DoArgs a) {
-  constexpr int N = 8, ACC = 1;
+  constexpr int N = 8;
   __shared__ __align__(16) T s_x[DO_THREADS / 32][256], s_r[RES ? DO_THREADS / 32 : 1][256];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const unsigned long long seed = __ldg(a.rng), offset = __ldg(a.rng + 1);
@@ -220,12 +220,12 @@ static __global__ void __launch_bounds__(DO_THREADS) sh_dropout_rows_kernel(cons
   T* sr = RES ? s_r[warp] + g * 8 * G : nullptr;
   // (a warp's groups go round together)
   const unsigned first = (blockIdx.x * (DO_THREADS / 32) + warp) << (5 - a.group_log);
-  ShRaw<T, ACC> x[N], res[N];
+  ShRaw<T, 1> x[N], res[N];
   auto fetch = [&](unsigned u) {
     const unsigned r = u / a.segs, c0 = (u - r * a.segs) * 8 * G;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const unsigned c = c0 + (i * G + j) * ACC;
+      const unsigned c = c0 + i * G + j;
       if (u < a.groups && c < (unsigned)a.cols) {
         x[i].load((const T*)a.x + (long long)r * a.xs + c);
         if constexpr (RES) res[i].load((const T*)a.residual + (long long)r * a.rs + c);
@@ -241,8 +241,8 @@ static __global__ void __launch_bounds__(DO_THREADS) sh_dropout_rows_kernel(cons
     float f[8], add[8];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      x[i].put(sx + (i * G + j) * ACC);
-      if constexpr (RES) res[i].put(sr + (i * G + j) * ACC);
+      x[i].put(sx + i * G + j);
+      if constexpr (RES) res[i].put(sr + i * G + j);
     }
     __syncwarp();
     ShRaw<T, 8> piece;
@@ -255,9 +255,9 @@ static __global__ void __launch_bounds__(DO_THREADS) sh_dropout_rows_kernel(cons
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const unsigned c = seg * 8 * G + (i * G + j) * ACC;
-      ShRaw<T, ACC> out;
-      out.take((const unsigned char*)(sx + (i * G + j) * ACC));
+      const unsigned c = seg * 8 * G + i * G + j;
+      ShRaw<T, 1> out;
+      out.take((const unsigned char*)(sx + i * G + j));
       if (u < a.groups && c < (unsigned)a.cols) out.put((T*)a.y + (long long)r * a.ys + c);
     }
     __syncwarp();

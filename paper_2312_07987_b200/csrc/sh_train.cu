@@ -139,10 +139,10 @@ int qn_lanes(int v, int d_head) {
 
 template <typename T, int V, int LANES, bool PAIRED, int NV = qn_vectors(V)>
 int qn_launch(const QnArgs& a, bool backward, bool pdl, int blocks, cudaStream_t st) {
-  if (!backward) return launch_k(pdl, sh_qk_norm_kernel<T, V, NV, LANES, PAIRED>, dim3((unsigned)blocks), dim3(QN_THREADS), 0, st, a);
-  const size_t sums = (size_t)(QN_THREADS / LANES) * a.D * 4;
-  if constexpr (V <= QN_BACKWARD_V) return launch_k(pdl, sh_qk_norm_backward_kernel<T, V, NV, LANES, PAIRED>, dim3((unsigned)blocks), dim3(QN_THREADS), sums, st, a);
-  return SH_ERR_UNSUPPORTED;                               // (vector_width gives the backward kernel no wider ones)
+  if constexpr (V <= QN_BACKWARD_V)                        // (vector_width gives the backward kernel no wider ones)
+    if (backward)
+      return launch_k(pdl, sh_qk_norm_backward_kernel<T, V, NV, LANES, PAIRED>, dim3((unsigned)blocks), dim3(QN_THREADS), (size_t)(QN_THREADS / LANES) * a.D * 4, st, a);
+  return launch_k(pdl, sh_qk_norm_kernel<T, V, NV, LANES, PAIRED>, dim3((unsigned)blocks), dim3(QN_THREADS), 0, st, a);
 }
 
 template <typename T, int V, bool PAIRED>

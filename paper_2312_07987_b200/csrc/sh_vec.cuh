@@ -24,26 +24,22 @@ struct ShRaw {
       w[0] = __ldcs(reinterpret_cast<const unsigned short*>(p));
     }
   }
-  __device__ __forceinline__ void take(const unsigned char* s) {             // from shared memory
+  __device__ __forceinline__ void take(const unsigned char* s) {             // from shared memory (one value, or 16 bytes and more)
     if constexpr (BYTES >= 16) {
 #pragma unroll
       for (int i = 0; i < BYTES / 16; ++i) {
         const uint4 v = reinterpret_cast<const uint4*>(s)[i];
         w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
       }
-    } else if constexpr (BYTES == 8) {
-      const uint2 v = *reinterpret_cast<const uint2*>(s);
-      w[0] = v.x; w[1] = v.y;
     } else if constexpr (BYTES == 4) {
       w[0] = *reinterpret_cast<const uint32_t*>(s);
     } else {
       w[0] = *reinterpret_cast<const unsigned short*>(s);
     }
   }
-  __device__ __forceinline__ void put(T* p) const {                          // as it is, anywhere (at most 8 bytes)
-    static_assert(BYTES <= 8, "");
-    if constexpr (BYTES == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
-    else if constexpr (BYTES == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
+  __device__ __forceinline__ void put(T* p) const {                          // one value, as it is
+    static_assert(V == 1, "");
+    if constexpr (BYTES == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
     else *reinterpret_cast<unsigned short*>(p) = (unsigned short)w[0];
   }
   __device__ __forceinline__ void fill(uint32_t word) {
