@@ -98,11 +98,13 @@ def test_a_refused_pass_leaves_the_one_before_it(layer, name):
 
 WITHOUT = """
 import torch
-for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"):
-    if hasattr(torch._C, name):
-        delattr(torch._C, name)
+names = {n: getattr(torch._C, n) for n in ("_cuda_getDevice", "_cuda_getCurrentRawStream") if hasattr(torch._C, n)}
+for n in names:
+    delattr(torch._C, n)
 from paper_2312_07987_b200 import binding as b
-assert b._current_device is torch.cuda.current_device
+for n, f in names.items():                                   # (torch.cuda's functions call them)
+    setattr(torch._C, n, f)
+assert b._current_device is torch.cuda.current_device and b._raw_stream is not names.get("_cuda_getCurrentRawStream")
 """
 
 
