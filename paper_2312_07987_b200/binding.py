@@ -207,12 +207,16 @@ class Layer:
         n = lib.sh_training_scratch_bytes(self.handle, which)
         return torch.empty(n, dtype=torch.uint8, device=self.workspace.device) if n else None, n
 
+    def _mine(self, t: Optional[torch.Tensor]) -> bool:
+        """Whether a tensor that the passes will read is on the layer's device (without a workspace the call itself is refused)."""
+        return t is None or (t.is_cuda and (self.workspace is None or t.device == self.workspace.device))
+
     def sh_set_qk_norm(self, gq=None, gk=None, eps: float = 1e-6, train: bool = True) -> None:
         """Q and K normalised per head between projection and attention (fp32 layers), gains gq, gk [d_head] fp32 device tensors or None;
         eps = 0 switches it off.  train: sh_backward returns dgq and dgk of the gains that are given."""
         D = self.dims[2]
         for g in (gq, gk):
-            assert g is None or (g.is_cuda and g.is_contiguous() and g.dtype == torch.float32 and tuple(g.shape) == (D,))
+            assert self._mine(g) and (g is None or (g.is_contiguous() and g.dtype == torch.float32 and tuple(g.shape) == (D,)))
         if ctypes.c_float(eps).value == 0.0:               # (as the call takes it; off: no gains, so no gradients of them)
             if eps != 0.0:
                 raise ValueError(f"eps must be 0 (off) or at least fp32's smallest positive value: got {eps}")
@@ -233,8 +237,9 @@ class Layer:
             self._settings.pop("balance", None)
             return None
         dev, (_, H, _, E, _) = self.workspace.device, self.dims
-        assert mask is None or (mask.is_cuda and mask.is_contiguous() and mask.dtype in (torch.bool, torch.uint8) and mask.numel() == self.batch * self.seq)
-        assert gloss is None or (gloss.is_cuda and gloss.dtype == torch.float32 and gloss.numel() == 1)
+        assert self._mine(mask) and self._mine(gloss), "mask and gloss must be on the layer's device"
+        assert mask is None or (mask.is_contiguous() and mask.dtype in (torch.bool, torch.uint8) and mask.numel() == self.batch * self.seq)
+        assert gloss is None or (gloss.dtype == torch.float32 and gloss.numel() == 1)
         sides = 1 if self.shared_selection else 2
         out = dict(loss=torch.empty((), device=dev), counts=torch.empty((sides, H, E), dtype=torch.int32, device=dev), prob=torch.empty((sides, H, E), device=dev))
         scratch, n = self._scratch(1)
@@ -244,7 +249,7 @@ class Layer:
 
     def sh_set_dropout(self, p: float, rng: Optional[torch.Tensor], train: bool = True) -> None:
         """Dropout of sh_forward's output (fp32 layers); rng: a device tensor of two int64, seed and offset, which the passes read (None: off)."""
-        assert rng is None or (rng.is_cuda and rng.dtype == torch.int64 and rng.is_contiguous() and rng.numel() == 2)
+        assert self._mine(rng) and (rng is None or rng.dtype == torch.int64 and rng.is_contiguous() and rng.numel() == 2)
         scratch, n = self._scratch(2) if train and rng is not None else (None, 0)
         _check(lib.sh_set_dropout(self.handle, p, _ptr(rng), _ptr(scratch), n))
         self._settings["dropout"] = (rng, scratch)

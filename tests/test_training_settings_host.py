@@ -2,6 +2,7 @@
 import os
 import subprocess
 import sys
+import types
 
 import pytest
 import torch
@@ -155,3 +156,18 @@ def test_other_outputs_that_overlap_are_refused():
     for stride in (63, 1, -63):
         f["y_stride"] = stride
         assert b.lib.sh_dropout(b._DROPOUT.pack(*[f[n] for n in given.DROPOUT]), None) == -1 and "share an address" in b.sh_last_error()
+
+
+def test_settings_want_tensors_of_the_layer_s_device(layer):
+    """Their pointers are kept, and read by kernels on that device."""
+    gain, rng, mask, one = device_tensor(32), device_tensor(2, dtype=torch.int64), device_tensor(16, dtype=torch.bool), device_tensor(1)
+    calls = (lambda: layer.sh_set_qk_norm(gain), lambda: layer.sh_set_qk_norm(None, gain), lambda: layer.sh_set_balance("counts", mask=mask),
+             lambda: layer.sh_set_balance("counts", gloss=one), lambda: layer.sh_set_dropout(0.1, rng))
+    for call in calls:
+        call()
+    layer.calls.clear()
+    layer.workspace = types.SimpleNamespace(device=torch.device("cuda", 1))
+    for call in calls:
+        with pytest.raises(AssertionError):
+            call()
+    assert not layer.calls
