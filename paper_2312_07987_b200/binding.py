@@ -142,6 +142,20 @@ def sh_last_error() -> str:
     return lib.sh_last_error().decode()
 
 
+class _Kept(tuple):
+    """The tensors of a training setting.  They were made on the stream that was current then; the passes may run on others."""
+
+    def used_on(self, stream) -> None:
+        """Their memory is not given to anybody before what `stream` holds now and later, until they are let go of, is done."""
+        streams = self.__dict__.setdefault("streams", set())
+        if stream.cuda_stream not in streams:
+            streams.add(stream.cuda_stream)
+            for t in self:
+                for one in t.values() if isinstance(t, dict) else (t,):
+                    if one is not None:
+                        one.record_stream(stream)
+
+
 class Layer:
     """Owns one sh_layer handle plus the torch tensors that back its workspace."""
 
@@ -226,7 +240,7 @@ class Layer:
         grads = [torch.empty_like(g) if g is not None and train else None for g in (gq, gk)]
         scratch, n = self._scratch(0) if train else (None, 0)
         _check(lib.sh_set_qk_norm(self.handle, _ptr(gq), _ptr(gk), eps, _ptr(grads[0]), _ptr(grads[1]), _ptr(scratch), n))
-        self._settings["qk_norm"] = (*grads, gq, gk, scratch)
+        self._settings["qk_norm"] = _Kept((*grads, gq, gk, scratch))
 
     def sh_set_balance(self, kind: Optional[str], coef: float = 0.01, mask: Optional[torch.Tensor] = None, gloss: Optional[torch.Tensor] = None) -> Optional[dict]:
         """sh_forward also gives the balance loss of its gates (fp32 layers): returns the tensors it writes, {loss, counts, prob}; sh_backward
@@ -244,7 +258,7 @@ class Layer:
         out = dict(loss=torch.empty((), device=dev), counts=torch.empty((sides, H, E), dtype=torch.int32, device=dev), prob=torch.empty((sides, H, E), device=dev))
         scratch, n = self._scratch(1)
         _check(lib.sh_set_balance(self.handle, SH_BALANCE[kind], coef, _ptr(mask), _ptr(out["loss"]), _ptr(out["counts"]), _ptr(out["prob"]), _ptr(gloss), _ptr(scratch), n))
-        self._settings["balance"] = (mask, gloss, out, scratch)
+        self._settings["balance"] = _Kept((mask, gloss, out, scratch))
         return out
 
     def sh_set_dropout(self, p: float, rng: Optional[torch.Tensor], train: bool = True) -> None:
@@ -252,12 +266,23 @@ class Layer:
         assert self._mine(rng) and (rng is None or rng.dtype == torch.int64 and rng.is_contiguous() and rng.numel() == 2)
         scratch, n = self._scratch(2) if train and rng is not None else (None, 0)
         _check(lib.sh_set_dropout(self.handle, p, _ptr(rng), _ptr(scratch), n))
-        self._settings["dropout"] = (rng, scratch)
+        self._settings["dropout"] = _Kept((rng, scratch))
 
     def sh_set_output_f16(self, enable: bool) -> None:
         """sh_forward writes fp16 instead of fp32 from now on (bf16 storage configuration only)."""
         _check(lib.sh_set_output_f16(self.handle, 1 if enable else 0))
         self.out_dtype = torch.float16 if enable else torch.float32
+
+    def _of_this_pass(self) -> None:
+        """The settings' tensors belong to the pass that has been made (a refused one leaves the pass before it, which keeps its own)."""
+        self._of_forward = dict(self._settings)
+        self._used_by_a_pass()
+
+    def _used_by_a_pass(self) -> None:
+        if self._of_forward:
+            stream = torch.cuda.current_stream()
+            for kept in self._of_forward.values():
+                kept.used_on(stream)
 
     def sh_forward(self, x: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         assert x.is_cuda and x.is_contiguous()
@@ -265,14 +290,14 @@ class Layer:
             out = torch.empty((x.shape[0], self.seq_out, x.shape[2]), dtype=getattr(self, "out_dtype", torch.float32), device=x.device)
         assert out.dtype == getattr(self, "out_dtype", torch.float32), "out must have the layer's output dtype (see sh_set_output_f16)"
         _check(lib.sh_forward(self.handle, _ptr(x), _ptr(out), _stream()))
-        self._of_forward = dict(self._settings)            # (a refused pass leaves the one before it, which keeps its tensors)
+        self._of_this_pass()
         return out
 
     def sh_forward_timed(self, x: torch.Tensor, out: torch.Tensor):
         """Returns the six stage times in ms: gate+sort, qk, v, attention, o, total."""
         ms = (ctypes.c_float * 6)()
         _check(lib.sh_forward_timed(self.handle, _ptr(x), _ptr(out), _stream(), ms))
-        self._of_forward = dict(self._settings)
+        self._of_this_pass()
         return list(ms)
 
     def sh_forward_stamped(self, x: torch.Tensor, out: torch.Tensor):
@@ -281,7 +306,7 @@ class Layer:
         n = len(STAMP_KERNELS)
         buf = (ctypes.c_uint64 * (3 * n))()
         _check(lib.sh_forward_stamped(self.handle, _ptr(x), _ptr(out), _stream(), buf))
-        self._of_forward = dict(self._settings)
+        self._of_this_pass()
         return {name: (buf[i], buf[n + i], buf[2 * n + i]) for i, name in enumerate(STAMP_KERNELS) if buf[2 * n + i] != 0}
 
     def sh_status_block(self):
@@ -307,6 +332,7 @@ class Layer:
         g = dict(dx=z(self.batch, self.seq, d_model), dWq=z(H, d_model, D), dWk=z(H, d_model, D), dWv=z(H, E, d_model, D),
                  dWo=z(H, E, D, d_model), dWs=z(H, d_model, E), dWd=z(H, d_model, E))
         _check(lib.sh_backward(self.handle, _ptr(x), _ptr(dout), *[_ptr(g[n]) for n in ("dx", "dWq", "dWk", "dWv", "dWo", "dWs", "dWd")], _stream()))
+        self._used_by_a_pass()
         for name, grad in zip(("dgq", "dgk"), self._of_forward.get("qk_norm", ())):
             if grad is not None:
                 g[name] = grad.clone()

@@ -335,3 +335,45 @@ def test_balance_sums_of_several_launches(S, H, E, ty):
     assert abs(float(got["loss"]) - loss) < S * H * (1 + float(torch.log(P).abs().max())) * off
     del z, idx
     torch.cuda.empty_cache()
+
+
+def test_memory_of_settings_waits_for_the_stream_of_their_passes():
+    """Set on one stream, used by passes on another: let go of while these wait to run, it is nobody else's yet."""
+    layer, x = tiny_layer()
+    G = torch.randn_like(x)
+    layer.sh_forward(x)
+    want = layer.sh_backward(x, G)
+    gains = [torch.rand(layer.dims[2], device="cuda") for _ in range(2)]
+    for turn in range(2):
+        layer.sh_set_qk_norm(*[g.clone() for g in gains])
+        layer.sh_set_balance("counts")
+        layer.sh_set_dropout(0.2, torch.tensor([1, 2], device="cuda"))
+        if turn == 0:
+            layer.sh_forward(x)
+            first = layer.sh_backward(x, G)
+            torch.cuda.synchronize()
+            continue
+        own = [t for kept in layer._settings.values() for t in kept if isinstance(t, torch.Tensor)]
+        places = {t.untyped_storage().data_ptr() for t in own}
+        sizes = [t.untyped_storage().nbytes() for t in own]
+        del own
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(400_000_000)                   # (a fifth of a second)
+            layer.sh_forward(x)
+            got = layer.sh_backward(x, G)
+        layer.sh_set_qk_norm(eps=0.0)
+        layer.sh_set_balance(None)
+        layer.sh_set_dropout(0.0, None)
+        with torch.cuda.stream(side):
+            layer.sh_forward(x)
+            plain = layer.sh_backward(x, G)
+        others = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(3)]
+        assert not side.query() and not places & {t.untyped_storage().data_ptr() for t in others}
+    side.synchronize()
+    for a, w in ((got, first), (plain, want)):
+        assert set(a) == set(w)
+        for n in w:
+            assert float((a[n] - w[n]).abs().max() / w[n].abs().max()) < 1e-4, n
+    layer.close()

@@ -33,6 +33,10 @@ def test_outputs_of_heads_keep_the_order_of_dimensions():
 class OnDevice(torch.Tensor):
     """A host tensor that passes for one on the device: what calls it is a stand-in for the library."""
     is_cuda = True
+    used = ()
+
+    def record_stream(self, stream):
+        self.used += (stream.cuda_stream,)
 
 
 def device_tensor(*shape, dtype=torch.float32):
@@ -51,6 +55,9 @@ def layer(monkeypatch):
         monkeypatch.setattr(b.lib, name, lambda *a, name=name: one.calls.append((name, a)) or (-1 if name in one.refuse else 0))
     monkeypatch.setattr(b.lib, "sh_training_scratch_bytes", lambda *a: 64)
     monkeypatch.setattr(b, "_stream", lambda: None)
+    one.stream = types.SimpleNamespace(cuda_stream=0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: one.stream)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, stream: None)
     return one
 
 
@@ -171,3 +178,18 @@ def test_settings_want_tensors_of_the_layer_s_device(layer):
         with pytest.raises(AssertionError):
             call()
     assert not layer.calls
+
+
+def test_settings_note_the_streams_of_their_passes(layer):
+    gain, rng, mask, x = device_tensor(32), device_tensor(2, dtype=torch.int64), device_tensor(16, dtype=torch.bool), device_tensor(2, 8, 128)
+    layer.sh_set_qk_norm(gain)
+    layer.sh_set_dropout(0.1, rng)
+    layer.sh_set_balance("counts", mask=mask)
+    for n, call in ((5, layer.sh_forward), (5, layer.sh_forward), (6, lambda x: layer.sh_backward(x, x)), (7, lambda x: layer.sh_forward_timed(x, x)), (8, lambda x: layer.sh_forward_stamped(x, x))):
+        layer.stream.cuda_stream = n
+        call(x)
+    assert all(t.used == (5, 6, 7, 8) for t in (gain, rng, mask))      # once each
+    layer.sh_set_dropout(0.2, device_tensor(2, dtype=torch.int64))
+    layer.stream.cuda_stream = 9
+    layer.sh_backward(x, x)                                            # of the pass before: with the tensors it had
+    assert rng.used == (5, 6, 7, 8, 9) and layer._settings["dropout"][0].used == ()
