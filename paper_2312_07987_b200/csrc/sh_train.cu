@@ -127,19 +127,22 @@ void qn_fill(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, QnA
 }
 
 constexpr int qn_vectors(int v) { return v >= 4 ? 2 : v == 2 ? 4 : 8; }
-// Vectors of two values and d_head 129 to 192: six to a lane, 16 lanes, where 32 with four each leave a third or more of them idle.
+// Vectors of two values and d_head 129 to 192: six to a lane, 16 lanes, where 32 with four each leave a third or more of them idle.  (20398 tokens, 10
+// heads each of queries and keys, six / four, us: 132 in halves, bf16, 80 / 117, backward 137 / 215; 190 next to one another 78 / 95, 114 / 162; fp32, 132 127 / 132, 190 140 / 136.
+// Not fp32 backward, whose rows on their way do not fit 128 registers then - 200 to 480 bytes of spills: 132 273 / 188, 190 230 / 191; 2048 tokens,
+// 4 heads each of 132, 11.2 / 10.8.)
 constexpr int QN_SIX = 6;
-bool qn_six(int v, int d_head) { return v == 2 && d_head > 128 && d_head <= 192; }
+bool qn_six(int v, int d_head, bool f32, bool backward) { return v == 2 && d_head > 128 && d_head <= 192 && !(f32 && backward); }
 // Lanes to a row: 4 to 32 (vectors of two values, where a quarter of the rotated width is odd, or less: 16 or 32).
-int qn_lanes(int v, int d_head) {
-  if (qn_six(v, d_head)) return 16;
+int qn_lanes(int v, int d_head, bool f32, bool backward) {
+  if (qn_six(v, d_head, f32, backward)) return 16;
   const int n = pow2_at_least((d_head + v * qn_vectors(v) - 1) / (v * qn_vectors(v))), least = v == 8 ? 4 : v == 4 ? 8 : 16;
   return n > least ? n : least;
 }
 
 template <typename T, int V, int LANES, bool PAIRED, int NV = qn_vectors(V)>
 int qn_launch(const QnArgs& a, bool backward, bool pdl, int blocks, cudaStream_t st) {
-  if constexpr (V <= QN_BACKWARD_V)                        // (vector_width gives the backward kernel no wider ones)
+  if constexpr (V <= QN_BACKWARD_V && !(NV == QN_SIX && sizeof(T) == 4))     // (vector_width gives the backward kernel no wider ones)
     if (backward)
       return launch_k(pdl, sh_qk_norm_backward_kernel<T, V, NV, LANES, PAIRED>, dim3((unsigned)blocks), dim3(QN_THREADS), (size_t)(QN_THREADS / LANES) * a.D * 4, st, a);
   return launch_k(pdl, sh_qk_norm_kernel<T, V, NV, LANES, PAIRED>, dim3((unsigned)blocks), dim3(QN_THREADS), 0, st, a);
@@ -149,7 +152,7 @@ template <typename T, int V, bool PAIRED>
 int qn_lanes_of(const QnArgs& a, int lanes, bool backward, bool pdl, int blocks, cudaStream_t st) {
   constexpr int LEAST = V == 8 ? 4 : V == 4 ? 8 : 16;
   if constexpr (V == 2)
-    if (qn_six(V, a.D)) return qn_launch<T, V, 16, PAIRED, QN_SIX>(a, backward, pdl, blocks, st);
+    if (qn_six(V, a.D, sizeof(T) == 4, backward)) return qn_launch<T, V, 16, PAIRED, QN_SIX>(a, backward, pdl, blocks, st);
   if (lanes == LEAST) return qn_launch<T, V, LEAST, PAIRED>(a, backward, pdl, blocks, st);
   if constexpr (LEAST < 16)
     if (lanes == 2 * LEAST) return qn_launch<T, V, 2 * LEAST, PAIRED>(a, backward, pdl, blocks, st);
@@ -174,7 +177,7 @@ int qn_run(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, bool 
   const int v = vector_width(p, back);
   QnArgs a;
   qn_fill(p, back, a);
-  const int lanes = qn_lanes(v, p.d_head), groups = QN_THREADS / lanes, most = p.q_heads > p.k_heads ? p.q_heads : p.k_heads;
+  const int lanes = qn_lanes(v, p.d_head, p.dtype == SH_F32, backward), groups = QN_THREADS / lanes, most = p.q_heads > p.k_heads ? p.q_heads : p.k_heads;
   // Heads to a group: all of them share a token's angles (16384 tokens, 40 heads of 128: 4 heads 64 us, 8 59, 16 64), but not so many that
   // SMs are left without a block (16 tokens, 8 heads: 4 heads 3.5 us, 1 2.7; 2048 tokens, 4 heads of 76, backward: 2 heads 6.3 us, 1 7.7).
   a.per = most < 8 ? (most < 1 ? 1 : most) : 8;
@@ -189,7 +192,7 @@ int qn_run(const sh_qk_norm_args& p, const sh_qk_norm_backward_args* back, bool 
   if (backward) {
     long long n[2];
     for (int i = 0; i < 2; ++i) n[i] = (items[i] + groups - 1) / groups;
-    const long long fit = (long long)sms * (p.dtype == SH_F32 ? qn_backward_blocks<float, 4, 2>() : v == 1 ? qn_backward_blocks<__half, 1, 8>() : qn_six(v, p.d_head) ? qn_backward_blocks<__half, 2, QN_SIX>() : qn_backward_blocks<__half, 4, 2>()), cap = fit < QN_MAX_BLOCKS ? fit : QN_MAX_BLOCKS;
+    const long long fit = (long long)sms * (p.dtype == SH_F32 ? qn_backward_blocks<float, 4, 2>() : v == 1 ? qn_backward_blocks<__half, 1, 8>() : qn_six(v, p.d_head, false, true) ? qn_backward_blocks<__half, 2, QN_SIX>() : qn_backward_blocks<__half, 4, 2>()), cap = fit < QN_MAX_BLOCKS ? fit : QN_MAX_BLOCKS;
     if (n[0] + n[1] > cap) {                               // shares by the sides' rows
       const long long all = n[0] + n[1];
       const long long b0 = n[0] ? (n[0] * cap + all / 2) / all : 0;

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2312_07987_b200 import binding, inputs
+from tests import test_gpu_training_operators as given
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
@@ -377,3 +378,10 @@ def test_memory_of_settings_waits_for_the_stream_of_their_passes():
         for n in w:
             assert float((a[n] - w[n]).abs().max() / w[n].abs().max()) < 1e-4, n
     layer.close()
+
+
+@pytest.mark.parametrize("ty", ["f32", "f16"])
+@pytest.mark.parametrize("D,R,halves", [(132, 132, True), (140, 140, True), (188, 100, True), (130, 130, False), (166, 60, False), (190, 190, False), (194, 194, False)])
+def test_norm_of_wide_heads_in_vectors_of_two(D, R, halves, ty):
+    for B, T, Hq, Hk in ((1, 1, 1, 1), (3, 17, 5, 2)):
+        given.test_norm_and_its_gradients((B, T, Hq, Hk, D, R, halves, "bthd", ty, 0.5), "packed")
