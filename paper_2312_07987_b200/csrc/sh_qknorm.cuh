@@ -12,7 +12,8 @@
 //
 // What bounds it: HBM forward (16384 tokens, 40 heads of 128 in bf16: 59 us, 5.7 TB/s of 6.56 measured; 16 heads in fp32: 45 us, 6.0), where a
 // group's heads are many; else what a group does once (angles, factors, addresses: as much as for three rows).  Backward, 16 heads: in
-// fp32 68 us, 5.9 TB/s; in bf16 42 us, 4.8 TB/s: a third of the instructions are sums across lanes, addresses and predicates, at 24 warps an SM.
+// fp32 68 us, 5.9 TB/s; in bf16 42 us, 4.8 TB/s: latency at 24 warps an SM - issue slots 62 % full, HBM 43 %, no warp ready in 37 % of the cycles; a
+// warp waits as long for the exchanges across lanes as for memory, and longest for the instruction before.
 // Rows in flight through shared memory (cp.async) instead of registers: 92 and 72 us.
 #pragma once
 #include "sh_vec.cuh"
@@ -21,7 +22,7 @@ constexpr int QN_THREADS = 256;
 constexpr int QN_MAX_D = 256;
 constexpr int QN_PAIRS = QN_MAX_D / 2;    // (as many as the widest row's lanes hold)
 // The backward kernel's vectors are of 4 values at most (8 of a 16-bit type: 128 registers and spills; 33.5 M values of 16384 tokens, 16 heads
-// of 128: 56 us, with 4 42), and its blocks 3 to an SM (fp32, whose rows on their way are twice as large, vectors of one value, and six of two: 2; 8 x 256
+// of 128: 56 us, with 4 42), and its blocks 3 to an SM, which leaves the paired variants of 16-bit types 16 to 60 bytes of spills (fp32, whose rows on their way are twice as large, vectors of one value, and six of two: 2; 8 x 256
 // tokens in fp32: 13.5 us with 3, 9.0 with 2).
 constexpr int QN_BACKWARD_V = 4;
 template <typename T, int V, int NV> __host__ __device__ constexpr int qn_backward_blocks() { return sizeof(T) == 4 || V == 1 || NV == 6 ? 2 : 3; }

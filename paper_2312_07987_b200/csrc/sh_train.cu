@@ -242,7 +242,8 @@ int bl_width(int dtype, int E) { return E <= 4 ? 4 : E <= 8 || dtype == SH_F32 ?
 
 // Few rows: one launch (sh_balance_small_kernel), which needs no workspace.  Up to 2^18 logits: 2048 tokens, 8 gates of 4 experts
 // 7.5 us on the device against 9.2, 14.2 against 17.6 with the host's part; 8192 tokens (2^18) 12.0 and 9.9, 14.3 and 17.6, of 16 experts (1024
-// tokens) 9.5 and 9.9; 2^19: 18 and 11, 19 and 18.
+// tokens) 9.5 and 9.9; 2^19: 18 and 11, 19 and 18.  (By the time of a call; the layer's passes, whose launches are chained, take the same rule, and from
+// 2^18 logits of few experts on they would do with the other kernel.)
 bool bl_small(long long tokens, long long gates, int E) {
   return gates <= BL_SMALL_GATES && gates * E <= BL_SMALL_COLS && tokens * gates * (E < 4 ? 4 : E) <= 1 << 18;
 }
