@@ -381,8 +381,8 @@ int sh_dropout(const sh_dropout_args* args, void* stream);
 
 /* The same as parts of the fp32 layer's own passes.  Host calls, no launch; they take effect with the next sh_forward, and end with
  * sh_configure / sh_set_workspace.  All pointers are device pointers of the caller, read or written by the passes: they stay
- * valid as long as the setting does, and until the last forward pass that had it has been differentiated (or another one
- * made).  A scratch holds sh_training_scratch_bytes(layer, which) bytes, aligned to 256, of one layer; sh_backward reads what
+ * valid as long as the setting does, until the last forward pass that had it has been differentiated (or another one made), and
+ * as long as a graph that captured such a pass is replayed.  A scratch holds sh_training_scratch_bytes(layer, which) bytes, aligned to 256, of one layer; sh_backward reads what
  * the forward pass left there (without it - where it may be NULL - sh_backward has no pass to differentiate).  sh_backward
  * differentiates the pass that was made, with its settings.  SH_ERR_UNSUPPORTED for bf16 storage and the dense
  * comparator. */

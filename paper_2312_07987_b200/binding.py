@@ -178,7 +178,7 @@ class Layer:
         self.workspace = None
         self.dtype = None
         self.batch = self.seq = 0
-        self._settings, self._of_forward = {}, {}
+        self._settings, self._of_forward, self._captured = {}, {}, {}
 
     def sh_configure(self, dtype: int, batch: int, seq: int, device="cuda", cache_len: int = 0) -> None:
         """cache_len > 0: Transformer-XL context (sh_configure_xl): x is [B, cache_len + seq, M], out [B, seq, M]."""
@@ -193,7 +193,8 @@ class Layer:
         base = self.workspace.data_ptr()
         self._ws_ptr = (base + 255) // 256 * 256
         self._settings = {}                                # tensors that the training settings read and write, by setting ...
-        self._of_forward = {}                              # ... and those of the last forward pass, which sh_backward differentiates
+        self._of_forward = {}                              # ... those of the last forward pass, which sh_backward differentiates ...
+        self._captured = {}                                # ... and those of captured passes
         _check(lib.sh_set_workspace(self.handle, ctypes.c_void_p(self._ws_ptr), nbytes))
 
     def sh_set_weights(self, Wq, Wk, Wv, Wo, Ws=None, Wd=None, bias_s=None, bias_d=None) -> None:
@@ -283,6 +284,8 @@ class Layer:
             stream = torch.cuda.current_stream()
             for kept in self._of_forward.values():
                 kept.used_on(stream)
+            if torch.cuda.is_current_stream_capturing():   # (a replay uses them whatever has been set since: kept until the next sh_configure)
+                self._captured.update({id(kept): kept for kept in self._of_forward.values()})
 
     def sh_forward(self, x: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         assert x.is_cuda and x.is_contiguous()

@@ -385,3 +385,32 @@ def test_memory_of_settings_waits_for_the_stream_of_their_passes():
 def test_norm_of_wide_heads_in_vectors_of_two(D, R, halves, ty):
     for B, T, Hq, Hk in ((1, 1, 1, 1), (3, 17, 5, 2)):
         given.test_norm_and_its_gradients((B, T, Hq, Hk, D, R, halves, "bthd", ty, 0.5), "packed")
+
+
+def test_a_captured_step_outlives_its_settings():
+    """Replayed after its settings have been switched off and their names taken by others, it still is the step that was captured."""
+    layer, x = tiny_layer()
+    G = torch.randn_like(x)
+    layer.sh_set_qk_norm(torch.rand(layer.dims[2], device="cuda"), torch.rand(layer.dims[2], device="cuda"))
+    layer.sh_set_balance("entropy", 0.1)
+    layer.sh_set_dropout(0.2, torch.tensor([1, 2], device="cuda"))
+    want = layer.sh_forward(x).clone(), layer.sh_backward(x, G)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = layer.sh_forward(x), layer.sh_backward(x, G)
+    layer.sh_set_qk_norm(eps=0.0)
+    layer.sh_set_balance(None)
+    layer.sh_set_dropout(0.0, None)
+    plain = layer.sh_forward(x).clone()
+    held = [torch.full((1 << n,), float("nan"), device="cuda") for n in range(4, 22) for _ in range(4)]
+    for _ in range(2):
+        graph.replay()
+        assert float((got[0] - want[0]).abs().max() / want[0].abs().max()) < 1e-5
+        assert set(got[1]) == set(want[1]) and "dgk" in got[1]
+        for n, w in want[1].items():
+            assert float((got[1][n] - w).abs().max() / w.abs().max()) < 1e-4, n
+        assert all(bool(h.isnan().all()) for h in held)
+        assert float((layer.sh_forward(x) - plain).abs().max() / plain.abs().max()) < 1e-5
+    layer.close()

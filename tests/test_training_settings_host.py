@@ -49,7 +49,7 @@ def layer(monkeypatch):
     one = object.__new__(b.Layer)
     one.handle, one.dense, one.shared_selection, one.dims = None, False, False, (128, 2, 32, 4, 2)
     one.workspace, one.dtype, one.batch, one.seq, one.seq_out = torch.empty(1), b.SH_F32, 2, 8, 8
-    one._settings, one._of_forward = {}, {}
+    one._settings, one._of_forward, one._captured = {}, {}, {}
     one.calls, one.refuse = [], set()
     for name in ("sh_set_qk_norm", "sh_set_balance", "sh_set_dropout", "sh_set_rope", "sh_forward", "sh_forward_timed", "sh_forward_stamped", "sh_backward"):
         monkeypatch.setattr(b.lib, name, lambda *a, name=name: one.calls.append((name, a)) or (-1 if name in one.refuse else 0))
@@ -57,6 +57,8 @@ def layer(monkeypatch):
     monkeypatch.setattr(b, "_stream", lambda: None)
     one.stream = types.SimpleNamespace(cuda_stream=0)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: one.stream)
+    one.capturing = False
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: one.capturing)
     monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, stream: None)
     return one
 
@@ -193,3 +195,22 @@ def test_settings_note_the_streams_of_their_passes(layer):
     layer.stream.cuda_stream = 9
     layer.sh_backward(x, x)                                            # of the pass before: with the tensors it had
     assert rng.used == (5, 6, 7, 8, 9) and layer._settings["dropout"][0].used == ()
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_settings_of_a_captured_pass_live_on(layer, backward):
+    """A replay uses them, whatever has been set since."""
+    x = device_tensor(2, 8, 128)
+    layer.sh_set_qk_norm(device_tensor(32))
+    layer.sh_set_dropout(0.1, device_tensor(2, dtype=torch.int64))
+    of_pass = list(layer._settings.values())
+    if backward:
+        layer.sh_forward(x)
+    assert not layer._captured
+    layer.capturing = True
+    layer.sh_backward(x, x) if backward else layer.sh_forward(x)
+    layer.capturing = False
+    layer.sh_set_qk_norm(eps=0.0)
+    layer.sh_set_dropout(0.0, None)
+    layer.sh_forward(x)
+    assert len(layer._captured) == 2 and all(any(k is kept for k in layer._captured.values()) for kept in of_pass)
